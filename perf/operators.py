@@ -32,13 +32,12 @@ def listed():
         # the down projection of the 12288-wide layer split over 8 devices, 4 sequences of 2048: the largest
         dict(name="linear_fwd_12288", op="linear_fwd", tokens=8192, d_in=6144, d_out=12288, type="bf16",
              act="none", bias=True, residual=True, save=False, pad=0),
-        # backward of the down projection that follows it, added to the gradients of earlier micro-batches
-        # in 32 bits
-        dict(name="linear_bwd_1024", op="linear_bwd", tokens=8192, d_in=4096, d_out=1024, type="bf16",
-             act="none", bias=True, grad32=True, pad=0),
+        # backward of the second case
+        dict(name="linear_bwd_1024", op="linear_bwd", tokens=8192, d_in=1024, d_out=4096, type="bf16",
+             act="gelu", bias=True, pad=0),
         # a short, ragged batch and a width that no 16-byte row stride fits
         dict(name="linear_bwd_ragged", op="linear_bwd", tokens=1537, d_in=768, d_out=2311, type="f16",
-             act="gelu", bias=True, grad32=False, pad=8),
+             act="relu", bias=True, pad=8),
         # a few tokens through the expert of the MoE-like workload: bound by its weights
         dict(name="ffn_fwd_few_tokens", op="ffn_fwd", tokens=7, d_in=2048, d_hidden=8192, type="bf16",
              act="silu", bias=False, residual=True, save=False, pad=0),
@@ -88,9 +87,6 @@ def draw(rng):
             case.update(type=rng.choice(("bf16", "f16", "f32")), kind=rng.choice(("layer", "rms")), post=post,
                         pre=not post or rng.random() < 0.7, gate=rng.random() < 0.5, residual=rng.random() < 0.8,
                         alpha=rng.choice((1.0, 0.75)), p=rng.choice((0.0, 0.1, 0.25)))
-        if op == "linear_bwd":      # with an activation its derivative is rounded to 16 bits on the way
-            case["grad32"] = case["act"] == "none" or rng.random() < 0.3
-            case["act"] = "none" if case["grad32"] else case["act"]
         if op in ("linear_fwd", "ffn_fwd"):
             case.update(residual=rng.random() < 0.5, save=rng.random() < 0.5)
         w = work(case)
@@ -107,9 +103,8 @@ def work(case):
         return {"bytes": e * n, "flops": 2 * t * d * f}
     if c["op"] == "linear_bwd":
         f = c["d_out"]
-        n = t * f * (1 + (c["act"] != "none")) + 2 * t * d + f * d
-        grads = 4 * (2 * f * d + f * c["bias"]) if c["grad32"] else e * (f * d + f * c["bias"])
-        return {"bytes": e * n + grads, "flops": 4 * t * d * f}
+        n = t * f * (1 + (c["act"] != "none")) + 2 * t * d + 2 * f * d + f * c["bias"]
+        return {"bytes": e * n, "flops": 4 * t * d * f}
     if c["op"] == "ffn_fwd":
         f = c["d_hidden"]
         n = t * d * (2 + c["residual"]) + 3 * f * d + (2 * f + d) * c["bias"] + 3 * t * f * c["save"]
@@ -155,10 +150,7 @@ def prepare(case, seed):
         else:
             s["dy"] = _normal(gen, t, f, ty, 0.5, pad=c["pad"])
             s["preact"] = _normal(gen, t, f, ty) if c["act"] != "none" else None
-            s["dweight_in"] = _normal(gen, f, d, torch.float32, 0.5 * t ** 0.5) if c["grad32"] else None
-            if c["grad32"]:
-                empty = functools.partial(empty, dtype=torch.float32)
-            s.update(dx=empty(t, d, dtype=ty), dweight=empty(f, d), dbias=empty(f) if c["bias"] else None)
+            s.update(dx=empty(t, d), dweight=empty(f, d), dbias=empty(f) if c["bias"] else None)
     elif c["op"].startswith("ffn"):
         f = c["d_hidden"]
         for name in ("w_gate", "w_up"):
@@ -287,9 +279,7 @@ def _plain(s, wide):
         return [y, z if c["save"] else None]
     if c["op"] == "linear_bwd":
         dz = v["dy"] if c["act"] == "none" else v["dy"] * _act_grad(v["preact"], c["act"])
-        dw = dz.T @ v["x"]
-        dw = dw + v["dweight_in"] if c["grad32"] else dw
-        return [dz @ v["weight"], dw, dz.sum(0) if c["bias"] else None]
+        return [dz @ v["weight"], dz.T @ v["x"], dz.sum(0) if c["bias"] else None]
     if c["op"] == "ffn_fwd":
         g, u = v["x"] @ v["w_gate"].T, v["x"] @ v["w_up"].T
         if c["bias"]:
@@ -346,8 +336,7 @@ def _framework(s):
         return [s["y"], s["preact"]]
     if c["op"] == "linear_bwd":
         engine.distsim_linear_backward(ctx, s["dy"], s["x"], s["weight"], dx=s["dx"], dweight=s["dweight"],
-                                       dbias=s["dbias"], preact=s["preact"], activation=c["act"],
-                                       dweight_in=s["dweight_in"])
+                                       dbias=s["dbias"], preact=s["preact"], activation=c["act"])
         return [s["dx"], s["dweight"], s["dbias"]]
     if c["op"] == "ffn_fwd":
         engine.distsim_gated_ffn_forward(ctx, s["x"], s["w_gate"], s["w_up"], s["w_down"], s["y"],
@@ -378,8 +367,7 @@ def run(state):
     if own:
         return _framework(state)
     ty = TYPES[state["case"]["type"]]
-    kinds = [ty, torch.float32, torch.float32] if state["case"].get("grad32") else [ty] * 7
-    return [None if v is None else v.to(k) for v, k in zip(_plain(state, torch.Tensor.float), kinds)]
+    return [None if v is None else v.to(ty) for v in _plain(state, torch.Tensor.float)]
 
 
 # ---------------------------------------------------------------- from the definitions, in 64 bits
@@ -449,8 +437,7 @@ def exact(case, seed):
         return [y + w["residual"] if c["residual"] else y, z if c["save"] else None]
     if c["op"] == "linear_bwd":
         dz = w["dy"] * _exact_act(w["preact"], c["act"])[1] if c["act"] != "none" else w["dy"]
-        dw = torch.einsum("tf,td->fd", dz, w["x"])
-        return [torch.einsum("tf,fd->td", dz, w["weight"]), dw + w["dweight_in"] if c["grad32"] else dw,
+        return [torch.einsum("tf,fd->td", dz, w["weight"]), torch.einsum("tf,td->fd", dz, w["x"]),
                 torch.einsum("tf->f", dz) if c["bias"] else None]
     if c["op"] == "ffn_fwd":
         g, u = affine(w["x"], w["w_gate"], w["b_gate"]), affine(w["x"], w["w_up"], w["b_up"])
