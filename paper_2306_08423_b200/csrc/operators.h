@@ -96,7 +96,8 @@ inline bool aligned_rows(const Matrix &x, int elem_bytes)
 {
     return (reinterpret_cast<uintptr_t>(x.p) & 15) == 0 && (x.ld * elem_bytes) % 16 == 0;
 }
-// Operands have aligned rows; for plan.pair so have in and out.  m, n >= 1, k[0] >= 1.
+// Operands have aligned rows; for plan.pair so have in and out, and the 16-byte piece that holds the last
+// column of an out row is written whole.  m, n >= 1, k[0] >= 1.
 cudaError_t launch_product(OperatorLaunch &l, const Product &p, const ProductPlan &plan);
 
 // Column-wise passes over [rows][cols] matrices of 16-bit types (column_kernels.cu).

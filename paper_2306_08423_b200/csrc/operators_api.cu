@@ -176,23 +176,26 @@ struct StandIn {
     size_t offset = 0;
     Matrix use{};
 
-    void plan(Call &c, bool needed)
+    // written: by tiled copies.  They write rows up to a 16-byte boundary (zeros behind the last column), so
+    // the caller's rows have to end on one: what follows a column range is not the operator's.
+    bool apart(bool written) const { return own.p && (!aligned_rows(own, elem) || (written && cols * elem % 16 != 0)); }
+    void plan(Call &c, bool needed, bool written = false)
     {
-        moved = needed && own.p && !aligned_rows(own, elem);
+        moved = needed && apart(written);
         if (moved) offset = c.room((size_t)rows * padded_ld(cols, elem) * elem);
     }
     void place(Call &c) { use = moved ? Matrix{c.at(offset), padded_ld(cols, elem)} : own; }
 };
-int64_t unaligned(std::initializer_list<const StandIn *> all)
+int64_t unaligned(std::initializer_list<const StandIn *> all, bool written)
 {
     int64_t bytes = 0;
     for (const StandIn *s : all)
-        if (s->own.p && !aligned_rows(s->own, s->elem)) bytes += s->rows * s->cols * s->elem;
+        if (s->apart(written)) bytes += s->rows * s->cols * s->elem;
     return bytes;
 }
 ProductPlan Call::plan(const Product &p, std::initializer_list<const StandIn *> in, std::initializer_list<const StandIn *> out) const
 {
-    return plan_of(p, unaligned(in), unaligned(out));
+    return plan_of(p, unaligned(in, false), unaligned(out, true));
 }
 Move move_of(const Matrix &dst, const Matrix &src, int64_t rows, int64_t cols, int elem)
 {
@@ -311,7 +314,8 @@ int distsim_linear_forward(distsim_ctx *ctx, void *stream, const distsim_linear 
     StandIn r = stand_in(o->residual, o->ld_residual, t, f, 2), y = stand_in(o->y, o->ld_y, t, f, 2), z = stand_in(o->preact, o->ld_preact, t, f, 2);
     const ProductPlan plan = c.plan(p, {&r}, {&y, &z});
     for (StandIn *s : {&x, &w}) s->plan(c, true);
-    for (StandIn *s : {&r, &y, &z}) s->plan(c, plan.pair);
+    r.plan(c, plan.pair);
+    for (StandIn *s : {&y, &z}) s->plan(c, plan.pair, true);
     if ((rc = c.reserve()) != DISTSIM_OK) return rc;
     for (StandIn *s : {&x, &w, &r, &y, &z}) s->place(c);
     p.a[0] = x.use;
@@ -358,8 +362,8 @@ int distsim_linear_backward(distsim_ctx *ctx, void *stream, const distsim_linear
     x.plan(c, o->dweight);
     w.plan(c, o->dx);
     dy.plan(c, !act && (o->dx || o->dweight));
-    dx.plan(c, plan_x.pair);
-    dw.plan(c, plan_w.pair);
+    dx.plan(c, plan_x.pair, true);
+    dw.plan(c, plan_w.pair, true);
     dwi.plan(c, plan_w.pair && o->dweight);
     const size_t dz_at = act ? c.room((size_t)t * padded_ld(f, 2) * 2) : 0;
     const size_t part_at = o->dbias ? c.room((size_t)column_pass_partials(f, c.l.sm_count) * 4) : 0;
@@ -436,9 +440,11 @@ int distsim_gated_ffn_forward(distsim_ctx *ctx, void *stream, const distsim_gate
     StandIn g = stand_in(o->gate, o->ld_gate, t, f, 2), u = stand_in(o->up, o->ld_up, t, f, 2);
     StandIn h = stand_in(o->hidden, o->ld_hidden, t, f, 2);
     const ProductPlan plan_h = c.plan(ph, {}, {&g, &u}), plan_y = c.plan(py, {&r}, {&y});
-    for (StandIn *s : {&x, &wg, &wu, &wd, &h}) s->plan(c, true);
-    for (StandIn *s : {&r, &y}) s->plan(c, plan_y.pair);
-    for (StandIn *s : {&g, &u}) s->plan(c, plan_h.pair);
+    for (StandIn *s : {&x, &wg, &wu, &wd}) s->plan(c, true);
+    h.plan(c, true, plan_h.pair);
+    r.plan(c, plan_y.pair);
+    y.plan(c, plan_y.pair, true);
+    for (StandIn *s : {&g, &u}) s->plan(c, plan_h.pair, true);
     const size_t h_at = o->hidden ? 0 : c.room((size_t)t * padded_ld(f, 2) * 2);
     if ((rc = c.reserve()) != DISTSIM_OK) return rc;
     for (StandIn *s : {&x, &wg, &wu, &wd, &h, &r, &y, &g, &u}) s->place(c);
@@ -507,9 +513,9 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     wd.plan(c, inner);
     for (StandIn *s : {&g, &u}) s->plan(c, inner && plan_i.pair);
     for (StandIn *s : {&wg, &wu}) s->plan(c, o->dx);
-    dx.plan(c, plan_x.pair);
-    for (StandIn *s : {&dwg, &dwu}) s->plan(c, plan_w.pair);
-    dwd.plan(c, plan_d.pair);
+    dx.plan(c, plan_x.pair, true);
+    for (StandIn *s : {&dwg, &dwu}) s->plan(c, plan_w.pair, true);
+    dwd.plan(c, plan_d.pair, true);
     const int64_t ld_i = padded_ld(f, 2);
     const size_t dg_at = inner ? c.room((size_t)t * ld_i * 2) : 0, du_at = inner ? c.room((size_t)t * ld_i * 2) : 0;
     const size_t part_at = o->db_gate || o->db_up || o->db_down

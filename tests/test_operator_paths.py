@@ -1,0 +1,54 @@
+"""Paths of the operators' kernels that the shapes of test_operators do not reach.  Plain implementations in
+64 bits and tolerances as there, unless a test derives its own."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from .test_operators import U32, close, ctx, ffn_case, linear_case, plan, randn, room  # noqa: E402, F401
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan", [0, -1, 1, -2], indirect=True)
+@pytest.mark.parametrize("shape", [(300, 72, 257, 143), (520, 131, 325, 3), (40, 65, 263, 1)])
+def test_rows_with_gaps_that_an_odd_width_leaves(ctx, plan, shape):
+    # rows that start on 16-byte boundaries and end off one: what lies between them is not the operator's
+    from paper_2306_08423_b200 import engine as E
+    t, d, f, gap = shape
+    rng = np.random.default_rng(t)
+    dt = torch.bfloat16
+    gap_d = -d % 8 + 8
+
+    def rows(n, cols, dtype=dt):
+        align = 16 // torch.empty((), dtype=dtype).element_size()
+        pad = gap if cols == f else gap_d
+        assert (cols + pad) % align == 0
+        return room(n, cols, dtype, pad, 0)
+    x, w, b, dy = linear_case(rng, t, d, f, 0, 0, dt)
+    (y, y_ok), (z, z_ok) = rows(t, f), rows(t, f)
+    E.distsim_linear_forward(ctx, x, w, y, bias=b, preact=z)
+    want = x.double() @ w.double().T + b.double()
+    for name, v in (("y", y), ("z", z)):
+        close(name, v, want, (d + 2) * U32 * (x.double().abs() @ w.double().abs().T + b.double().abs()))
+    for ok in (y_ok, z_ok):
+        ok()
+    for grad in (dt, torch.float32):
+        (dx, dx_ok), (dw, dw_ok) = rows(t, d), rows(f, d, grad)
+        E.distsim_linear_backward(ctx, dy, x, w, dx=dx, dweight=dw)
+        close("dx", dx, dy.double() @ w.double(), (f + 2) * U32 * dy.double().abs() @ w.double().abs())
+        close("dw", dw, dy.double().T @ x.double(), (t + 2) * U32 * dy.double().abs().T @ x.double().abs())
+        dx_ok()
+        dw_ok()
+    o = ffn_case(rng, t, d, f, 0, 0, dt)
+    out = {n: rows(t, f) for n in ("hidden", "gate", "up")}
+    out["y"] = rows(t, d)
+    E.distsim_gated_ffn_forward(ctx, **o, **{n: q[0] for n, q in out.items()}, activation="none")
+    h = out["hidden"][0].double()
+    close("y", out["y"][0], h @ o["w_down"].double().T, (f + 3) * U32 * (h.abs() @ o["w_down"].double().abs().T))
+    grads = dict(dx=rows(t, d), dw_gate=rows(f, d), dw_up=rows(f, d), dw_down=rows(d, f))
+    dy = randn(rng, t, d, dtype=dt)
+    E.distsim_gated_ffn_backward(ctx, dy, **o, hidden=out["hidden"][0], gate=out["gate"][0], up=out["up"][0],
+                                 **{n: q[0] for n, q in grads.items()}, activation="none")
+    close("dw_down", grads["dw_down"][0], dy.double().T @ h, (t + 2) * U32 * dy.double().abs().T @ h.abs())
+    for _, ok in (*out.values(), *grads.values()):
+        ok()
