@@ -48,7 +48,7 @@ extern "C" {
 enum {
     DISTSIM_OK = 0,
     DISTSIM_E_ARG = -1,        /* null pointer, malformed table or space            */
-    DISTSIM_E_STATE = -2,      /* table or space not loaded yet                     */
+    DISTSIM_E_STATE = -2,      /* table or space not loaded yet; not in a capture   */
     DISTSIM_E_RANGE = -3,      /* candidate index outside [0, n_candidates)         */
     DISTSIM_E_CAPACITY = -4,   /* caller's output buffer too small                  */
     DISTSIM_E_OVERFLOW = -5,   /* a time or count bound does not fit 62 bits        */
@@ -379,10 +379,15 @@ int distsim_topk_static(void *stream, const int64_t *d_batch_ns, int64_t first, 
  *     and activations are 32-bit floats; each output is rounded once from them.
  *   - Outputs do not overlap inputs unless stated.  No tokens (0) is a valid size: outputs of
  *     that many rows are empty and parameter gradients are zero (or their *_in).
- *   - Asynchronous on `stream`.  Scratch belongs to the context and grows on first use (not
- *     possible while a stream is captured: make one call of that size before).  A call that
+ *   - Asynchronous on `stream`.  Scratch belongs to the context and grows on first use.  While a
+ *     call is captured it cannot grow, nor can a context's first call be captured
+ *     (DISTSIM_E_STATE, with nothing captured: make one call of that size before).  A call that
  *     uses scratch on another stream than the one that used it last waits for that one on the
- *     device; inside a capture the caller orders them.
+ *     device.  A captured call waits for none, and a replay is a use of the scratch that the
+ *     context does not see: the caller orders replays after the calls before them, and the
+ *     context's next calls and replays after them.  Scratch that a captured call uses stays where
+ *     it is until the context is destroyed; its graphs may be replayed up to then, whatever larger
+ *     calls come between.
  *   - Kernels wait for copies and products a bounded number of times.  A wait that gives up
  *     leaves that call's outputs undefined; the context's next operator call, and
  *     distsim_operator_status, return DISTSIM_E_TIMEOUT.

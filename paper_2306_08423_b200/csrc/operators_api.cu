@@ -21,6 +21,9 @@ struct OperatorState {
     cudaEvent_t done = nullptr;                  // behind the last call's kernels
     cudaStream_t last = nullptr;
     bool used = false;
+    bool captured = false;                       // a captured call uses the scratch: graphs hold its address
+    struct Retired { void *block; Retired *next; };
+    Retired *retired = nullptr;                  // earlier blocks that graphs may still hold
     int sm_count = 0;
     int32_t forced_plan = 0;                     // testing hook, see distsim_testing.h
     bool ready = false;
@@ -28,6 +31,11 @@ struct OperatorState {
     ~OperatorState()
     {
         if (scratch) cudaFree(scratch);
+        while (Retired *r = retired) {
+            cudaFree(r->block);
+            retired = r->next;
+            delete r;
+        }
         if (counters) cudaFree(counters);
         if (status) cudaFreeHost(status);
         if (done) cudaEventDestroy(done);
@@ -53,6 +61,7 @@ struct Call {
     OperatorAccess a{};
     OperatorLaunch l{};
     cudaStream_t stream;
+    bool capturing = false;
     size_t need = 0;
 
     explicit Call(distsim_ctx *c, void *s) : ctx(c), stream(static_cast<cudaStream_t>(s)) {}
@@ -72,7 +81,11 @@ struct Call {
         cudaError_t e = cudaSetDevice(a.device);
         if (e != cudaSuccess) return cuda(e, "cudaSetDevice");
         OperatorState &s = *a.state;
+        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
+        if ((e = cudaStreamIsCapturing(stream, &cap)) != cudaSuccess) return cuda(e, "stream");
+        capturing = cap != cudaStreamCaptureStatusNone;
         if (!s.ready) {
+            if (capturing) return fail(DISTSIM_E_STATE, "the first operator call of a context cannot be captured");
             if ((!s.counters && (e = cudaMalloc(&s.counters, kColumnCounters * sizeof(int32_t))) != cudaSuccess) ||
                 (e = cudaMemset(s.counters, 0, kColumnCounters * sizeof(int32_t))) != cudaSuccess ||
                 (e = cudaStreamSynchronize(nullptr)) != cudaSuccess ||
@@ -131,33 +144,33 @@ struct Call {
         cudaError_t e;
         if (need == 0) return DISTSIM_OK;
         if (need > s.capacity) {
-            // cudaFree waits for the kernels that still use the old block
-            if (s.scratch) cudaFree(s.scratch);
+            if (capturing) return fail(DISTSIM_E_STATE, "operator scratch cannot grow while a call is captured: make one call of this size before");
+            if (s.scratch && s.captured) {
+                auto *r = new (std::nothrow) OperatorState::Retired{s.scratch, s.retired};
+                if (!r) return fail(DISTSIM_E_CUDA, "out of host memory");
+                s.retired = r;
+            } else if (s.scratch && (e = cudaFree(s.scratch)) != cudaSuccess) {          // waits for the kernels that still use it
+                return cuda(e, "operator scratch");
+            }
             s.scratch = nullptr;
             s.capacity = 0;
+            s.captured = false;
             if ((e = cudaMalloc(&s.scratch, need)) != cudaSuccess) { s.scratch = nullptr; return cuda(e, "operator scratch"); }
             s.capacity = need;
         }
-        if (s.used && s.last != stream) {
-            cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-            if ((e = cudaStreamIsCapturing(stream, &cap)) != cudaSuccess) return cuda(e, "stream");
-            if (cap == cudaStreamCaptureStatusNone && (e = cudaStreamWaitEvent(stream, s.done, 0)) != cudaSuccess) return cuda(e, "stream order");
-        }
+        if (capturing) s.captured = true;
+        else if (s.used && s.last != stream && (e = cudaStreamWaitEvent(stream, s.done, 0)) != cudaSuccess) return cuda(e, "stream order");
         return DISTSIM_OK;
     }
     int end(cudaError_t e)
     {
         *a.launches += l.launches;
         if (e != cudaSuccess) return cuda(e, "operator launch");
-        if (need == 0) return DISTSIM_OK;
+        if (need == 0 || capturing) return DISTSIM_OK;
         OperatorState &s = *a.state;
-        cudaStreamCaptureStatus cap = cudaStreamCaptureStatusNone;
-        if ((e = cudaStreamIsCapturing(stream, &cap)) != cudaSuccess) return cuda(e, "stream");
-        if (cap == cudaStreamCaptureStatusNone) {
-            if ((e = cudaEventRecord(s.done, stream)) != cudaSuccess) return cuda(e, "stream order");
-            s.last = stream;
-            s.used = true;
-        }
+        if ((e = cudaEventRecord(s.done, stream)) != cudaSuccess) return cuda(e, "stream order");
+        s.last = stream;
+        s.used = true;
         return DISTSIM_OK;
     }
 };

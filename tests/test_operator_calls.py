@@ -1,0 +1,118 @@
+"""The host side of an operator call - scratch, order between streams, captures, devices - on a CUDA
+runtime without a device (fake_cuda_runtime.cpp): no GPU needed."""
+import ctypes as C
+import os
+import re
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+E_ARG, E_STATE, E_CUDA = -1, -2, -6
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    """The library on the fake runtime."""
+    from paper_2306_08423_b200 import build as B
+    B.build()
+    so = str(tmp_path_factory.mktemp("fake") / "libdistsim_fake.so")
+    objects = [os.path.join(B._OBJ, s.replace(".cu", ".o")) for s in B.SOURCES]
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-I/usr/local/cuda/include", "-o", so,
+                    os.path.join(HERE, "fake_cuda_runtime.cpp"), *objects], check=True, capture_output=True, text=True)
+    from paper_2306_08423_b200 import operators as O
+    f = C.CDLL(so)
+    f.distsim_create.argtypes = [C.POINTER(C.c_void_p), C.c_int]
+    f.distsim_destroy.argtypes = [C.c_void_p]
+    f.distsim_last_error.argtypes = [C.c_void_p]
+    f.distsim_last_error.restype = C.c_char_p
+    f.distsim_operator_status.argtypes = [C.c_void_p, C.c_void_p]
+    f.distsim_testing_set_product_plan.argtypes = [C.c_void_p, C.c_int32]
+    for name, struct in (("linear", O._Linear), ("gated_ffn", O._GatedFfn), ("residual_norm", O._ResidualNorm)):
+        for way in ("forward", "backward"):
+            getattr(f, f"distsim_{name}_{way}").argtypes = [C.c_void_p, C.c_void_p, C.POINTER(struct)]
+    f.fake_log.restype = C.c_char_p
+    f.fake_stream.argtypes = [C.c_void_p, C.c_ulonglong, C.c_int]
+    return f
+
+
+class Context:
+    def __init__(self, lib, device=0):
+        self.lib, self.h = lib, C.c_void_p()
+        assert lib.distsim_create(C.byref(self.h), device) == 0
+
+    def close(self):
+        self.lib.distsim_destroy(self.h)
+
+    def backward(self, tokens, stream, d_in=64, d_out=128, rc=0):
+        """A linear backward pass, which needs scratch that grows with the tokens."""
+        from paper_2306_08423_b200 import operators as O
+        o = O._Linear(tokens=tokens, d_in=d_in, d_out=d_out, activation=O.ACTIVATIONS["gelu"])
+        for k, name in enumerate(("x", "weight", "preact", "dy", "dx", "dweight", "dbias")):
+            setattr(o, name, (0x7000 + k) << 32)
+            if name != "dbias":
+                setattr(o, "ld_" + name, d_out if name in ("preact", "dy") else d_in)
+        assert self.lib.distsim_linear_backward(self.h, stream, C.byref(o)) == rc, self.error()
+
+    def error(self):
+        return self.lib.distsim_last_error(self.h).decode()
+
+
+@pytest.fixture
+def ctx(lib):
+    c = Context(lib)
+    for handle in (0x10, 0x20, 0x30):
+        lib.fake_stream(handle, handle, 0)
+    log(lib)
+    yield c
+    c.close()
+    log(lib)
+
+
+def log(lib):
+    return lib.fake_log().decode().splitlines()
+
+
+def of(events, word):
+    """The events of a kind; of allocations and frees their blocks."""
+    found = [e for e in events if e.startswith(word)]
+    return [re.search(r"block=(\S+)", e)[1] for e in found] if word in ("malloc", "free") else found
+
+
+# ---------------------------------------------------------------- scratch and captures
+
+def test_scratch_of_a_captured_call_stays(lib):
+    ctx = Context(lib)
+    before = lib.fake_blocks()
+    log(lib)
+    ctx.backward(100, 0x10)
+    small = of(log(lib), "malloc")[-1]
+    lib.fake_stream(0x20, 2, 1)
+    ctx.backward(100, 0x20)                          # the graph holds addresses of this block
+    lib.fake_stream(0x20, 2, 0)
+    ctx.backward(10000, 0x10)
+    events = log(lib)
+    large = of(events, "malloc")
+    assert len(large) == 1 and small not in of(events, "free")
+    ctx.backward(20000, 0x10)                        # no graph holds that one
+    events = log(lib)
+    assert of(events, "free") == large and len(of(events, "malloc")) == 1
+    ctx.close()
+    assert small in of(log(lib), "free")
+    assert lib.fake_blocks() < before                # nothing stays behind
+
+
+def test_scratch_does_not_grow_in_a_capture(lib, ctx):
+    lib.fake_stream(0x20, 2, 1)
+    ctx.backward(100, 0x20, rc=E_STATE)              # a context's first call sets its state up
+    assert "captured" in ctx.error() and not log(lib)
+    lib.fake_stream(0x20, 2, 0)
+    ctx.backward(100, 0x10)
+    lib.fake_stream(0x20, 2, 1)
+    log(lib)
+    ctx.backward(10000, 0x20, rc=E_STATE)
+    assert "captured" in ctx.error() and not log(lib)
+    ctx.backward(90, 0x20)                           # the block that was there still serves
+    events = log(lib)
+    assert of(events, "launch") and not of(events, "malloc")
+    lib.fake_stream(0x20, 2, 0)

@@ -52,3 +52,50 @@ def test_rows_with_gaps_that_an_odd_width_leaves(ctx, plan, shape):
     close("dw_down", grads["dw_down"][0], dy.double().T @ h, (t + 2) * U32 * dy.double().abs().T @ h.abs())
     for _, ok in (*out.values(), *grads.values()):
         ok()
+
+
+@pytest.mark.gpu
+def test_replay_after_a_larger_call():
+    # a graph's scratch stays when a later call needs more; on a context of its own, whose scratch is that small
+    from paper_2306_08423_b200 import engine as E
+    c = E.Context(0)
+    try:
+        rng = np.random.default_rng(6)
+        t, d, f = 700, 136, 264
+        x, w, _, dy = linear_case(rng, t, d, f, 1, 1, torch.bfloat16)
+        z = randn(rng, t, f, dtype=torch.bfloat16)
+
+        def outputs():
+            return [torch.full(s, 7.0, dtype=torch.bfloat16, device="cuda") for s in ((t, d), (f, d), (f,))]
+
+        def run(o):
+            E.distsim_linear_backward(c, dy, x, w, dx=o[0], dweight=o[1], dbias=o[2], preact=z, activation="gelu")
+        eager, replayed = outputs(), outputs()
+        run(eager)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            run(replayed)
+        large = linear_case(rng, 9000, 640, 1032, 1, 1, torch.bfloat16)
+        out = [torch.empty(9000, 640, dtype=torch.bfloat16, device="cuda"), torch.empty(1032, 640, dtype=torch.bfloat16, device="cuda")]
+        E.distsim_linear_backward(c, large[3], large[0], large[1], dx=out[0], dweight=out[1], preact=large[3], activation="gelu")
+        other = torch.full((1 << 26,), float("nan"), device="cuda")      # takes what has been freed
+        for _ in range(2):
+            for v in replayed:
+                v.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(eager, replayed))
+        assert bool(torch.isnan(other).all())
+        # a call that a capture cannot hold is refused before anything is captured
+        wider = linear_case(rng, 30000, 640, 1032, 1, 1, torch.bfloat16)
+        graph = torch.cuda.CUDAGraph()
+        out = torch.empty(30000, 640, dtype=torch.bfloat16, device="cuda")
+        with torch.cuda.graph(graph):
+            with pytest.raises(E.DistsimError, match="captured") as e:
+                E.distsim_linear_backward(c, wider[3], wider[0], wider[1], dx=out, preact=wider[3], activation="gelu")
+            replayed[2].zero_()
+        assert e.value.code == E.E_STATE
+        E.distsim_linear_backward(c, wider[3], wider[0], wider[1], dx=out, preact=wider[3], activation="gelu")
+        assert bool(torch.isfinite(out).all())
+    finally:
+        c.close()
