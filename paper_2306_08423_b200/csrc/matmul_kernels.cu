@@ -1101,21 +1101,23 @@ bool encode(CUtensorMap *map, CUtensorMapDataType type, int elem, const Matrix &
 template <int EPI, int ACT, class T, bool WIDE>
 cudaError_t launch_pair(OperatorLaunch &l, const ProductParams &p)
 {
-    static const cudaError_t set = cudaFuncSetAttribute(pair_product_kernel<EPI, ACT, T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kPairSmem);
-    if (set != cudaSuccess) return set;
+    const auto kernel = pair_product_kernel<EPI, ACT, T, WIDE>;
+    const cudaError_t e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), kPairSmem);
+    if (e != cudaSuccess) return e;
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.groups;
     const int64_t pairs = tiles < l.sm_count / 2 ? tiles : l.sm_count / 2;
-    return launch_kernel(l, kEarly, pair_product_kernel<EPI, ACT, T, WIDE>, (unsigned)(2 * pairs), 1, kPairThreads, kPairSmem, 0, p);
+    return launch_kernel(l, kEarly, kernel, (unsigned)(2 * pairs), 1, kPairThreads, kPairSmem, 0, p);
 }
 
 template <int EPI, class T, bool WIDE>
 cudaError_t launch(OperatorLaunch &l, const ProductParams &p, const ProductPlan &plan)
 {
+    cudaError_t e;
     if (plan.few) {
         if constexpr (!WIDE) {
-            static const cudaError_t set = cudaFuncSetAttribute(few_rows_kernel<EPI, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewSmem);
-            if (set != cudaSuccess) return set;
-            return launch_kernel(l, kEarly, few_rows_kernel<EPI, T>, (unsigned)(2 * p.tiles_n * plan.split), 1, kFewThreads, kFewSmem, 2 * plan.split, p);
+            const auto kernel = few_rows_kernel<EPI, T>;
+            if ((e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), kFewSmem)) != cudaSuccess) return e;
+            return launch_kernel(l, kEarly, kernel, (unsigned)(2 * p.tiles_n * plan.split), 1, kFewThreads, kFewSmem, 2 * plan.split, p);
         }
     }
     if (plan.pair) {
@@ -1128,11 +1130,11 @@ cudaError_t launch(OperatorLaunch &l, const ProductParams &p, const ProductPlan 
         default: return launch_pair<EPI, DISTSIM_ACT_NONE, T, WIDE>(l, p);
         }
     }
-    static const cudaError_t set = cudaFuncSetAttribute(split_product_kernel<EPI, T, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem);
-    if (set != cudaSuccess) return set;
+    const auto kernel = split_product_kernel<EPI, T, WIDE>;
+    if ((e = ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), kSplitSmem)) != cudaSuccess) return e;
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n * p.groups;
     if (tiles * plan.split > 0x3fffffff) return cudaErrorInvalidConfiguration;
-    return launch_kernel(l, kEarly, split_product_kernel<EPI, T, WIDE>, (unsigned)(2 * tiles * plan.split), 1, kSplitThreads, kSplitSmem, 2 * plan.split, p);
+    return launch_kernel(l, kEarly, kernel, (unsigned)(2 * tiles * plan.split), 1, kSplitThreads, kSplitSmem, 2 * plan.split, p);
 }
 
 template <class T>
@@ -1149,50 +1151,44 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 }  // namespace
 
-// Clusters of 2 split blocks of the split kernel that the device holds at a time (its other
-// instances take the same room).
-int64_t split_capacity(int split, int sm_count)
+int split_capacity(int split, int sm_count)
 {
-    static int known[5] = {};
-    if (!known[split]) {
-        const auto kernel = split_product_kernel<kEpiLinear, __nv_bfloat16, false>;
-        cudaLaunchConfig_t cfg{};
-        cudaLaunchAttribute attr[1];
-        cfg.gridDim = dim3((unsigned)(2 * split * sm_count));
-        cfg.blockDim = dim3(kSplitThreads);
-        cfg.dynamicSmemBytes = kSplitSmem;
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)(2 * split);
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSplitSmem) != cudaSuccess ||
-            cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
-            cudaGetLastError();
-            n = sm_count / (2 * split) > 1 ? sm_count / (2 * split) * 3 / 4 : 1;
-        }
-        known[split] = n;
+    const auto kernel = split_product_kernel<kEpiLinear, __nv_bfloat16, false>;       // the others take the same room
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    cfg.gridDim = dim3((unsigned)(2 * split * sm_count));
+    cfg.blockDim = dim3(kSplitThreads);
+    cfg.dynamicSmemBytes = kSplitSmem;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)(2 * split);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int n = 0;
+    if (ensure_dynamic_smem(reinterpret_cast<const void *>(kernel), kSplitSmem) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = sm_count / (2 * split) > 1 ? sm_count / (2 * split) * 3 / 4 : 1;
     }
-    return known[split];
+    return n;
 }
 
 bool few_rows(const Product &p) { return p.m <= kFewRows && !p.a_mn && !p.wide && p.groups == 1; }
 
-ProductPlan choose_plan(const Product &p, int sm_count, int64_t unaligned_in, int64_t unaligned_out)
+ProductPlan choose_plan(const Product &p, const OperatorLaunch &l, int64_t unaligned_in, int64_t unaligned_out)
 {
     ProductPlan plan;
     const int64_t steps = ceil_div(p.k[0], 64) + ceil_div(p.k[1], 64);
     const int64_t tiles = ceil_div(p.m, 256) * ceil_div(p.n, p.epilogue == kEpiGated ? 128 : 256) * p.groups;
     const double rows = p.m < 128 ? p.m / 128.0 : 1.0;
-    const int64_t waves = ceil_div(tiles, sm_count / 2);
+    const int64_t waves = ceil_div(tiles, l.sm_count / 2);
     plan.pair = true;
     double best = 4.7 + 1.1 * rows + 0.265 * (double)(waves * steps) + (waves > 1 ? 3.0 : 0.0);
     if (unaligned_in + unaligned_out > 0) best += 2.0 + (double)(unaligned_in + unaligned_out) / 2.3e6;
     const double direct = (double)unaligned_out / 3.8e6 + (double)unaligned_in / 0.6e6;
     for (int s = 1; s <= 4 && s <= steps; s *= 2) {
         const double wave = (s == 1 ? 4.2 : s == 2 ? 4.7 : 5.2) + 4.3 * rows + 0.265 * (double)ceil_div(steps, s);
-        const double t = wave * (double)ceil_div(tiles, split_capacity(s, sm_count)) + direct;
+        const double t = wave * (double)ceil_div(tiles, l.split_capacity[s / 2]) + direct;
         if (t < best) { best = t; plan.pair = false; plan.split = s; }
     }
     if (few_rows(p)) {
@@ -1202,7 +1198,7 @@ ProductPlan choose_plan(const Product &p, int sm_count, int64_t unaligned_in, in
         plan.pair = false;
         plan.split = 1;
         const int64_t columns = ceil_div(p.n, p.epilogue == kEpiGated ? 128 : 256);
-        for (int s = 2; s <= 4 && s <= steps && columns * s <= sm_count; s *= 2) plan.split = s;
+        for (int s = 2; s <= 4 && s <= steps && columns * s <= l.sm_count; s *= 2) plan.split = s;
     }
     return plan;
 }

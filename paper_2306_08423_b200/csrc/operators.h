@@ -42,6 +42,7 @@ struct Product {
 struct OperatorLaunch {
     cudaStream_t stream = nullptr;
     int sm_count = 0;
+    const int *split_capacity = nullptr;         // of the device, for splits of 1, 2, 4
     int32_t *status = nullptr;    // host-mapped word that a kernel whose wait gave up writes
     int64_t launches = 0;
 };
@@ -89,7 +90,9 @@ bool few_rows(const Product &p);
 // copies (2.3 MB a us); the others write them value by value (3.8 MB a us) and read them so (0.6 MB a
 // us).  Measured, persistent / split 1 in us: 6969 x 56 x 925 14.6 / 20.8, with a residual 21.4 / 35.3;
 // 8192 x 1024 x 4097 79.6 / 119, with a residual 109 / 243; 1537 x 2304 x 771 19.7 / 15.5 (split 2).
-ProductPlan choose_plan(const Product &p, int sm_count, int64_t unaligned_in, int64_t unaligned_out);
+ProductPlan choose_plan(const Product &p, const OperatorLaunch &l, int64_t unaligned_in, int64_t unaligned_out);
+// Clusters of `split` pairs of the split kernel that the current device holds at a time.
+int split_capacity(int split, int sm_count);
 
 // 16-byte aligned rows, as the tiled copies need them.
 inline bool aligned_rows(const Matrix &x, int elem_bytes)

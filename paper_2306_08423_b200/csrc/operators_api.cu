@@ -25,6 +25,7 @@ struct OperatorState {
     struct Retired { void *block; Retired *next; };
     Retired *retired = nullptr;                  // earlier blocks that graphs may still hold
     int sm_count = 0;
+    int split_capacity[3] = {};                  // of the context's device, see operators.h
     int32_t forced_plan = 0;                     // testing hook, see distsim_testing.h
     bool ready = false;
 
@@ -94,6 +95,7 @@ struct Call {
                 (!s.done && (e = cudaEventCreateWithFlags(&s.done, cudaEventDisableTiming)) != cudaSuccess) ||
                 (e = cudaDeviceGetAttribute(&s.sm_count, cudaDevAttrMultiProcessorCount, a.device)) != cudaSuccess)
                 return cuda(e, "operator set-up");
+            for (int i = 0; i < 3; ++i) s.split_capacity[i] = split_capacity(1 << i, s.sm_count);
             *s.status = 0;
             s.ready = true;
         }
@@ -101,6 +103,7 @@ struct Call {
         if (rc != DISTSIM_OK) return rc;
         l.stream = stream;
         l.sm_count = s.sm_count;
+        l.split_capacity = s.split_capacity;
         l.status = s.d_status;
         return DISTSIM_OK;
     }
@@ -118,7 +121,7 @@ struct Call {
     ProductPlan plan_of(const Product &p, int64_t unaligned_in, int64_t unaligned_out) const
     {
         const int32_t f = a.state->forced_plan;
-        if (f == 0) return choose_plan(p, l.sm_count, unaligned_in, unaligned_out);
+        if (f == 0) return choose_plan(p, l, unaligned_in, unaligned_out);
         ProductPlan q;
         q.pair = f == -1;
         q.few = f <= -2 && few_rows(p);

@@ -116,3 +116,32 @@ def test_scratch_does_not_grow_in_a_capture(lib, ctx):
     events = log(lib)
     assert of(events, "launch") and not of(events, "malloc")
     lib.fake_stream(0x20, 2, 0)
+
+
+# ---------------------------------------------------------------- devices
+
+def test_products_on_two_devices(lib):
+    # a kernel's limit on shared memory belongs to the device: every kind of product runs on both
+    contexts = [Context(lib, d) for d in (0, 1)]
+    for plan in (-1, 1, 2, 4, -2):
+        for c in contexts:
+            assert lib.distsim_testing_set_product_plan(c.h, plan) == 0
+            log(lib)
+            c.backward(40, 0x10)
+            assert len(of(log(lib), "launch")) == 3
+    for c in contexts:
+        c.close()
+
+
+def test_choice_of_kernel_goes_by_the_contexts_device(lib):
+    # dx has 4 x 4 tiles with a reduction of 4096: split where the device holds clusters enough
+    kinds = []
+    for held in (70, 1):
+        lib.fake_clusters(held)
+        c = Context(lib, len(kinds))
+        log(lib)
+        c.backward(1000, 0x10, d_in=1024, d_out=4096)
+        kinds.append(of(log(lib), "launch")[1])          # behind the column pass
+        c.close()
+    lib.fake_clusters(10)
+    assert "split_product" in kinds[0] and "pair_product" in kinds[1], kinds
