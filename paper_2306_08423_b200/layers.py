@@ -86,6 +86,12 @@ def time_layer(ctx, tokens, hidden, d_hidden, gated=False, p=0.1, repeats=5):
     """(forward, backward) device time of a shard in ns: the median of ``repeats`` replays of each
     captured pass after three, with the L2 cache overwritten before it, by CUDA events."""
     import torch
+    with torch.cuda.device(ctx.device):              # streams, captures and events are those of the current device
+        return _time_layer(ctx, tokens, hidden, d_hidden, gated, p, repeats)
+
+
+def _time_layer(ctx, tokens, hidden, d_hidden, gated, p, repeats):
+    import torch
     layer = FeedForward(ctx, tokens, hidden, d_hidden, gated=gated, p=p)
     device = f"cuda:{ctx.device}"
     y, h, dy, dh = (torch.randn(tokens, hidden, device=device).to(torch.bfloat16) for _ in range(4))

@@ -145,3 +145,34 @@ def test_choice_of_kernel_goes_by_the_contexts_device(lib):
         c.close()
     lib.fake_clusters(10)
     assert "split_product" in kinds[0] and "pair_product" in kinds[1], kinds
+
+
+def test_a_layer_is_timed_on_the_contexts_device(monkeypatch):
+    # streams, captures and events are those of PyTorch's current device: the timing takes the context's for it
+    import torch
+    from paper_2306_08423_b200 import layers
+    now = [0]
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, now[0] = now[0], self.device
+
+        def __exit__(self, *_):
+            now[0] = self.before
+
+    class Built(Exception):
+        pass
+
+    def build(ctx, *a, **k):
+        raise Built(now[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(layers, "FeedForward", build)
+
+    class Second:
+        device = 1
+    with pytest.raises(Built) as e:
+        layers.time_layer(Second, 8, 64, 128)
+    assert e.value.args == (1,) and now == [0]
