@@ -10,7 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 
-from ._library import OK, _lib, _stream
+from ._library import OK, _lib
 
 OPERATOR_EXPORTS = ("distsim_operator_status", "distsim_linear_forward", "distsim_linear_backward",
                     "distsim_gated_ffn_forward", "distsim_gated_ffn_backward",
@@ -146,7 +146,7 @@ def _sizes(t, name):
 
 def distsim_operator_status(ctx, stream=None) -> None:
     """Waits for ``stream``; raises if a kernel of an earlier operator call gave up waiting."""
-    ctx._check(_lib.distsim_operator_status(ctx._h, _stream(stream)))
+    ctx._check(_lib.distsim_operator_status(ctx._h, _raw_stream(ctx.device) if stream is None else stream.cuda_stream))
 
 
 def distsim_linear_forward(ctx, x, weight, y, bias=None, residual=None, preact=None, activation="none", stream=None) -> None:

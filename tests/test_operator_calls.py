@@ -176,3 +176,19 @@ def test_a_layer_is_timed_on_the_contexts_device(monkeypatch):
     with pytest.raises(Built) as e:
         layers.time_layer(Second, 8, 64, 128)
     assert e.value.args == (1,) and now == [0]
+
+
+def test_status_waits_for_the_contexts_device(lib, ctx, monkeypatch):
+    # without a stream: PyTorch's current one of the context's device, as the operators themselves take it
+    from paper_2306_08423_b200 import operators as O
+    monkeypatch.setattr(O, "_lib", lib)
+    monkeypatch.setattr(O, "_raw_stream", {0: 0x10, 1: 0x20}.__getitem__)
+
+    class Second:
+        device, _h = 1, ctx.h
+
+        @staticmethod
+        def _check(rc):
+            assert rc == 0
+    O.distsim_operator_status(Second)
+    assert of(log(lib), "synchronize") == ["synchronize device=0 stream=0x20"]
