@@ -19,7 +19,7 @@ struct OperatorState {
     int32_t *status = nullptr;                   // host memory that the device writes
     int32_t *d_status = nullptr;
     cudaEvent_t done = nullptr;                  // behind the last call's kernels
-    cudaStream_t last = nullptr;
+    unsigned long long last = 0;                 // that call's stream, by its id: a later stream may get its handle
     bool used = false;
     bool captured = false;                       // a captured call uses the scratch: graphs hold its address
     struct Retired { void *block; Retired *next; };
@@ -63,6 +63,7 @@ struct Call {
     OperatorLaunch l{};
     cudaStream_t stream;
     bool capturing = false;
+    unsigned long long stream_id = 0;            // where scratch is used, outside a capture
     size_t need = 0;
 
     explicit Call(distsim_ctx *c, void *s) : ctx(c), stream(static_cast<cudaStream_t>(s)) {}
@@ -161,8 +162,12 @@ struct Call {
             if ((e = cudaMalloc(&s.scratch, need)) != cudaSuccess) { s.scratch = nullptr; return cuda(e, "operator scratch"); }
             s.capacity = need;
         }
-        if (capturing) s.captured = true;
-        else if (s.used && s.last != stream && (e = cudaStreamWaitEvent(stream, s.done, 0)) != cudaSuccess) return cuda(e, "stream order");
+        if (capturing) {
+            s.captured = true;
+            return DISTSIM_OK;
+        }
+        if ((e = cudaStreamGetId(stream, &stream_id)) != cudaSuccess) return cuda(e, "stream");
+        if (s.used && s.last != stream_id && (e = cudaStreamWaitEvent(stream, s.done, 0)) != cudaSuccess) return cuda(e, "stream order");
         return DISTSIM_OK;
     }
     int end(cudaError_t e)
@@ -172,7 +177,7 @@ struct Call {
         if (need == 0 || capturing) return DISTSIM_OK;
         OperatorState &s = *a.state;
         if ((e = cudaEventRecord(s.done, stream)) != cudaSuccess) return cuda(e, "stream order");
-        s.last = stream;
+        s.last = stream_id;
         s.used = true;
         return DISTSIM_OK;
     }

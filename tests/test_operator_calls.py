@@ -192,3 +192,28 @@ def test_status_waits_for_the_contexts_device(lib, ctx, monkeypatch):
             assert rc == 0
     O.distsim_operator_status(Second)
     assert of(log(lib), "synchronize") == ["synchronize device=0 stream=0x20"]
+
+
+# ---------------------------------------------------------------- order between streams
+
+def test_calls_on_several_streams_wait_for_each_other(lib, ctx):
+    ctx.backward(100, 0x10)
+    log(lib)
+    for stream, waits in ((0x10, 0), (0x20, 1), (0x20, 0), (0x10, 1)):
+        ctx.backward(100, stream)
+        events = log(lib)
+        assert len(of(events, "wait")) == waits, events
+        assert not waits or events[0] == f"wait stream={stream:#x}"
+        assert events[-1] == f"record stream={stream:#x}"
+
+
+def test_a_stream_with_an_earlier_ones_handle_waits(lib, ctx):
+    # a stream is destroyed with work pending, and the next one gets its handle; the per-thread handle is another
+    # stream in every thread
+    ctx.backward(100, 0x10)
+    log(lib)
+    lib.fake_stream(0x10, 77, 0)
+    ctx.backward(100, 0x10)
+    assert log(lib)[0] == "wait stream=0x10"
+    ctx.backward(100, 0x10)
+    assert not of(log(lib), "wait")
