@@ -173,13 +173,17 @@ struct Call {
     int end(cudaError_t e)
     {
         *a.launches += l.launches;
+        cudaError_t order = cudaSuccess;
+        if (need > 0 && !capturing) {                        // after a failure too: what was launched before it uses the scratch
+            OperatorState &s = *a.state;
+            order = cudaEventRecord(s.done, stream);
+            if (order == cudaSuccess) {
+                s.last = stream_id;
+                s.used = true;
+            }
+        }
         if (e != cudaSuccess) return cuda(e, "operator launch");
-        if (need == 0 || capturing) return DISTSIM_OK;
-        OperatorState &s = *a.state;
-        if ((e = cudaEventRecord(s.done, stream)) != cudaSuccess) return cuda(e, "stream order");
-        s.last = stream_id;
-        s.used = true;
-        return DISTSIM_OK;
+        return order == cudaSuccess ? DISTSIM_OK : cuda(order, "stream order");
     }
 };
 

@@ -217,3 +217,15 @@ def test_a_stream_with_an_earlier_ones_handle_waits(lib, ctx):
     assert log(lib)[0] == "wait stream=0x10"
     ctx.backward(100, 0x10)
     assert not of(log(lib), "wait")
+
+
+def test_a_call_that_fails_half_way_is_waited_for(lib, ctx):
+    ctx.backward(100, 0x10)
+    log(lib)
+    lib.fake_fail_launch(2)
+    ctx.backward(100, 0x20, rc=E_CUDA)
+    assert "operator launch" in ctx.error()
+    events = log(lib)
+    assert len(of(events, "launch")) == 2 and events[-1] == "record stream=0x20"
+    ctx.backward(100, 0x10)
+    assert log(lib)[0] == "wait stream=0x10"
