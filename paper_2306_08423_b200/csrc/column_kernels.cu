@@ -25,7 +25,8 @@ constexpr int kMinRows = 32;                     // rows a block takes at least
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Runs of rows that a column range is cut into: as many blocks as run at a time.
+// Runs of rows that a column range is cut into: as many blocks as run at a time.  Several (which are
+// counted) only where the ranges are half as many at most: fewer than kColumnCounters.
 int64_t row_runs(int64_t rows, int64_t ranges, int sm_count)
 {
     int64_t runs = (int64_t)sm_count * kBlocksPerSm / ranges;
@@ -240,17 +241,6 @@ cudaError_t column_pass(OperatorLaunch &l, const ColumnPass &c)
         exact = exact && q.cols % 8 == 0 && aligned_rows(q.x, 2);
     }
     if (p.n == 0) return cudaSuccess;
-    if (ranges > kColumnCounters && p.part[0].sums) {
-        if (p.n == 1) return cudaErrorInvalidConfiguration;
-        for (const ColumnPass::Part &q : c.part) {           // each by itself
-            ColumnPass one = c;
-            for (ColumnPass::Part &o : one.part) o = ColumnPass::Part{};
-            one.part[0] = q;
-            const cudaError_t e = q.x.p ? column_pass<T, ACT>(l, one) : cudaSuccess;
-            if (e != cudaSuccess) return e;
-        }
-        return cudaSuccess;
-    }
     p.z = (const T *)c.z.p;
     p.ld_z = c.z.ld;
     p.out = (T *)const_cast<void *>(c.out.p);

@@ -99,3 +99,25 @@ def test_replay_after_a_larger_call():
         assert bool(torch.isfinite(out).all())
     finally:
         c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("grad", [torch.bfloat16, torch.float32])
+def test_bias_gradients_of_more_than_a_million_columns(ctx, grad):
+    from paper_2306_08423_b200 import engine as E
+    t, d, f, dt = 5, 16, 2 ** 20 + 300, torch.bfloat16
+    rng = np.random.default_rng(8)
+    x, w, dy = randn(rng, t, d, dtype=dt), randn(rng, f, d, dtype=dt), randn(rng, t, f, dtype=dt)
+    db, dx = torch.full((f,), 7.0, dtype=grad, device="cuda"), torch.empty_like(x)
+    E.distsim_linear_backward(ctx, dy, x, w, dx=dx, dbias=db)
+    close("db", db, dy.double().sum(0), (t + 2) * U32 * dy.double().abs().sum(0))
+    close("dx", dx, dy.double() @ w.double(), (f + 2) * U32 * dy.double().abs() @ w.double().abs())
+    # no activation: du = dh g, dg = dh u, rounded to 2^-8 at the most
+    g, u, dy, wd = randn(rng, t, f, dtype=dt), dy, x, randn(rng, d, f, dtype=dt)
+    grads = [torch.full((n,), 7.0, dtype=grad, device="cuda") for n in (f, f, d)]
+    E.distsim_gated_ffn_backward(ctx, dy, x, w, w, wd, None, g, u, db_gate=grads[0], db_up=grads[1], db_down=grads[2], activation="none")
+    dh = dy.double() @ wd.double()
+    dh_off = (d + 2) * U32 * dy.double().abs() @ wd.double().abs()
+    for name, got, other in (("db_gate", grads[0], u.double()), ("db_up", grads[1], g.double())):
+        close(name, got, (dh * other).sum(0), ((2.0 ** -8 + (t + 2) * U32) * (dh * other).abs() + 2 * dh_off * other.abs()).sum(0))
+    close("db_down", grads[2], dy.double().sum(0), (t + 2) * U32 * dy.double().abs().sum(0))
