@@ -1,11 +1,13 @@
 """Paths of the operators' kernels that the shapes of test_operators do not reach.  Plain implementations in
 64 bits and tolerances as there, unless a test derives its own."""
+import math
+
 import numpy as np
 import pytest
 
 torch = pytest.importorskip("torch")
 
-from .test_operators import U32, close, ctx, ffn_case, linear_case, plan, randn, room  # noqa: E402, F401
+from .test_operators import U32, act64, close, ctx, ffn_case, linear_case, plan, randn, room  # noqa: E402, F401
 
 
 @pytest.mark.gpu
@@ -121,3 +123,39 @@ def test_bias_gradients_of_more_than_a_million_columns(ctx, grad):
     for name, got, other in (("db_gate", grads[0], u.double()), ("db_up", grads[1], g.double())):
         close(name, got, (dh * other).sum(0), ((2.0 ** -8 + (t + 2) * U32) * (dh * other).abs() + 2 * dh_off * other.abs()).sum(0))
     close("db_down", grads[2], dy.double().sum(0), (t + 2) * U32 * dy.double().abs().sum(0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan", [-1, 1, -2], indirect=True)
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_negative_tails_of_activations(ctx, plan, act):
+    """Values and slopes far below zero are products of small numbers, to a relative error: exponentials of arguments
+    up to 2^7 in powers of two, rounded twice (2^7 2^-23 ln 2), and ten further roundings of 2^-23."""
+    from paper_2306_08423_b200 import engine as E
+    e = 2.0 ** 7 * U32 * math.log(2) + 10 * U32
+    lowest = {"gelu": -12.0, "gelu_tanh": -9.0, "silu": -60.0}[act]
+    z = torch.linspace(lowest, -1.5, 8 * 40, device="cuda").bfloat16().view(40, 8)
+    eye = torch.eye(8, device="cuda").bfloat16()
+    y, dx = torch.empty_like(z), torch.empty_like(z)
+    E.distsim_linear_forward(ctx, z, eye, y, activation=act)
+    want, slope = act64(z.double(), act)
+    if act == "gelu":                                # 1 + erf cancels in 64 bits as well
+        want = 0.5 * z.double() * torch.special.erfc(-z.double() / math.sqrt(2))
+        slope = want / z.double() + z.double() * torch.exp(-z.double().square() / 2) / math.sqrt(2 * math.pi)
+    elif act == "gelu_tanh":
+        k = math.sqrt(8 / math.pi)
+        s = torch.sigmoid(k * (z.double() + 0.044715 * z.double() ** 3))
+        want = z.double() * s
+        slope = s + want * (1 - s) * k * (1 + 0.134145 * z.double().square())
+    bad = (y.double() - want).abs() > (2.0 ** -8 + e) * want.abs()
+    assert not bad.any(), (z[bad], y[bad], want[bad])
+    # the slope's two terms have opposite signs; by the preceding value, dz = slope (dy = 1), rounded on its way to dx
+    E.distsim_linear_backward(ctx, torch.ones_like(z), z, eye, dx=dx, preact=z, activation=act)
+    terms = (want / z.double()).abs() * (1 + 2 * z.double().abs() * (1 + z.double().square()))
+    bad = (dx.double() - slope).abs() > (2.0 ** -8 + e) * slope.abs() + e * terms
+    assert not bad.any(), (z[bad], dx[bad], slope[bad])
+    if act == "gelu":                                # at the ends: z, 0, and no number for none
+        z[0, :3] = torch.tensor([math.inf, -math.inf, math.nan], device="cuda").bfloat16()
+        E.distsim_linear_forward(ctx, z.T.contiguous(), torch.eye(40, device="cuda").bfloat16()[:1], y.view(-1)[:8].view(8, 1), activation=act)
+        ends = y.view(-1)[:3]
+        assert ends[0] == math.inf and ends[1] == 0 and torch.isnan(ends[2])
