@@ -154,7 +154,10 @@ __device__ __forceinline__ void activation_both(Pair z, Pair &value, Pair &slope
         const Pair z2 = mul2(z, z);
         const Pair s = logistic(mul2(z, fma2(both(0.0713548162726f), z2, both(1.59576912160573f))));
         value = mul2(z, s);
-        slope = fma2(fma2(value, mul2(s, both(-1.f)), value), fma2(both(0.2140644488178f), z2, both(1.59576912160573f)), s);
+        // from |z| = 100 on s is 0 or 1 and the first factor zero: z^2 stays finite
+        const float2 f = halves(z2);
+        const Pair cut = make_pair2(fminf(f.x, 1e4f), fminf(f.y, 1e4f));
+        slope = fma2(fma2(value, mul2(s, both(-1.f)), value), fma2(both(0.2140644488178f), cut, both(1.59576912160573f)), s);
     } else if (ACT == DISTSIM_ACT_SILU) {
         const Pair s = logistic(z);
         value = mul2(z, s);

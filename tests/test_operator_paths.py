@@ -159,3 +159,21 @@ def test_negative_tails_of_activations(ctx, plan, act):
         E.distsim_linear_forward(ctx, z.T.contiguous(), torch.eye(40, device="cuda").bfloat16()[:1], y.view(-1)[:8].view(8, 1), activation=act)
         ends = y.view(-1)[:3]
         assert ends[0] == math.inf and ends[1] == 0 and torch.isnan(ends[2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan", [-1, 1, -2], indirect=True)
+@pytest.mark.parametrize("act", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_slopes_of_arguments_whose_square_is_infinite(ctx, plan, act):
+    # they are 1 and 0, and the values z and 0
+    from paper_2306_08423_b200 import engine as E
+    z = torch.tensor([3e38, 1e20, 2e19, 1e4, 200.0, -3e38, -1e20, -200.0], device="cuda").bfloat16().expand(16, 8).contiguous()
+    eye = torch.eye(8, device="cuda").bfloat16()
+    dx, dg = torch.empty_like(z), torch.empty_like(z)
+    E.distsim_linear_backward(ctx, torch.ones_like(z), z, eye, dx=dx, preact=z, activation=act)
+    up = (z > 0).to(z.dtype)
+    assert torch.equal(dx, up)
+    # the gated block's: dx = dg + du, dh = 1, u = 1
+    du = torch.where(z > 0, z, torch.zeros_like(z))
+    E.distsim_gated_ffn_backward(ctx, torch.ones_like(z), z, eye, eye, eye, None, z, torch.ones_like(z), dx=dg, activation=act)
+    assert torch.equal(dg, (up.float() + du.float()).bfloat16())
