@@ -410,7 +410,7 @@ int distsim_operator_status(distsim_ctx *ctx, void *stream);
  *              dbias = sum of dz over the tokens.  (The residual's gradient is dy.)
  * Nullable: bias, residual, preact (forward: z is not kept), dx, dweight, dweight_in, dbias.
  * dtype: DISTSIM_BF16 or DISTSIM_F16.  dz is rounded to it when an activation is given (it is an
- * operand of the products).
+ * operand of the products); dbias is summed before that.
  */
 typedef struct {
     int64_t tokens, d_in, d_out;
@@ -438,7 +438,8 @@ int distsim_linear_backward(distsim_ctx *ctx, void *stream, const distsim_linear
  *   backward   dh = dy w_down;  dg = dh * u * activation'(g);  du = dh * activation(g)  (one kernel)
  *              dx = dg w_gate + du w_up;  dw_gate = dg^T x;  dw_up = du^T x;  dw_down = dy^T h;
  *              db_gate, db_up, db_down = sums of dg, du, dy over the tokens
- * h, dg and du are rounded to dtype (they are operands of the next products).
+ * h, dg and du are rounded to dtype (they are operands of the next products); db_gate and db_up are
+ * summed before that.
  * Nullable: the biases, residual; forward: hidden, gate, up (gate and up together); backward: any
  * gradient.  dtype: DISTSIM_BF16 or DISTSIM_F16.
  */

@@ -36,10 +36,10 @@ int64_t row_runs(int64_t rows, int64_t ranges, int sm_count)
 
 template <class T>
 struct PassParams {
-    int64_t rows;
     struct {
         const T *x;
-        int64_t ld, cols;
+        const float *partials;                   // instead of x
+        int64_t ld, cols, rows;
         void *sums;
         int first;                               // column range
     } part[kPassParts];
@@ -62,7 +62,7 @@ column_pass_kernel(const __grid_constant__ PassParams<T> p)
     while (k + 1 < p.n && (int)blockIdx.x >= p.part[k + 1].first) ++k;
     const T *const x = p.part[k].x, *const z = p.z;
     T *const out = p.out;
-    const int64_t ld_x = p.part[k].ld, ld_z = p.ld_z, ld_out = p.ld_out, cols = p.part[k].cols, rows = p.rows;
+    const int64_t ld_x = p.part[k].ld, ld_z = p.ld_z, ld_out = p.ld_out, cols = p.part[k].cols, rows = p.part[k].rows;
     const int64_t start = (int64_t)((int)blockIdx.x - p.part[k].first) * kColsPerBlock, col = start + lane * 8;
     const int valid = (int)min(cols - col, (int64_t)8);
     const int64_t r0 = rows * blockIdx.y / gridDim.y, r1 = rows * (blockIdx.y + 1) / gridDim.y;
@@ -73,7 +73,17 @@ column_pass_kernel(const __grid_constant__ PassParams<T> p)
     constexpr int kRowsAhead = (ACT == DISTSIM_ACT_NONE ? 4 : 2) / (EXACT ? 1 : 2);      // rows a warp loads at a time
     grid_let_next();
     grid_wait();
-    if (valid > 0)
+    if (ACT == DISTSIM_ACT_NONE && p.part[k].partials) {
+        if (valid > 0)
+#pragma unroll 4
+            for (int64_t r = r0 + warp; r < r1; r += 8) {
+                const float4 *from = reinterpret_cast<const float4 *>(p.part[k].partials + r * ld_x + col);
+                const float4 a = from[0], b = from[1];
+                const Pair v[4] = {make_pair2(a.x, a.y), make_pair2(a.z, a.w), make_pair2(b.x, b.y), make_pair2(b.z, b.w)};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) sum.v[i] = add2(sum.v[i], v[i]);
+            }
+    } else if (valid > 0)
         // some rows at a time: their loads are under way together
         for (int64_t r = r0 + warp; r < r1; r += 8 * kRowsAhead) {
             Request<EXACT> a[kRowsAhead], b[kRowsAhead];
@@ -228,17 +238,20 @@ cudaError_t column_pass(OperatorLaunch &l, const ColumnPass &c)
     PassParams<T> p{};
     int64_t ranges = 0;
     bool exact = (!c.z.p || aligned_rows(c.z, 2)) && (!c.out.p || aligned_rows(c.out, 2));
-    p.rows = c.rows;
+    int64_t rows = 0;
     for (const ColumnPass::Part &q : c.part) {
         if (!q.x.p) continue;
         auto &to = p.part[p.n++];
-        to.x = (const T *)q.x.p;
+        if (q.partials) to.partials = (const float *)q.x.p;
+        else to.x = (const T *)q.x.p;
         to.ld = q.x.ld;
         to.cols = q.cols;
+        to.rows = q.partials ? q.partials : c.rows;
+        rows = to.rows > rows ? to.rows : rows;
         to.sums = q.sums;
         to.first = (int)ranges;
         ranges += ceil_div(q.cols, kColsPerBlock);
-        exact = exact && q.cols % 8 == 0 && aligned_rows(q.x, 2);
+        exact = exact && (q.partials || (q.cols % 8 == 0 && aligned_rows(q.x, 2)));
     }
     if (p.n == 0) return cudaSuccess;
     p.z = (const T *)c.z.p;
@@ -250,7 +263,7 @@ cudaError_t column_pass(OperatorLaunch &l, const ColumnPass &c)
     p.partial = c.partial;
     p.counters = c.counters;
     return launch_kernel(l, kEarly, exact ? column_pass_kernel<T, ACT, true> : column_pass_kernel<T, ACT, false>, (unsigned)ranges,
-                         (unsigned)row_runs(c.rows, ranges, l.sm_count), 256, 0, 0, p);
+                         (unsigned)row_runs(rows, ranges, l.sm_count), 256, 0, 0, p);
 }
 
 template <class T>

@@ -84,6 +84,8 @@ struct alignas(64) ProductParams {
     const void *in_p[2];
     void *out_p[3];
     int64_t in_ld[2], out_ld[3];
+    float *sums[2];                              // kEpiGatedBack: see Product::sums
+    int64_t sums_ld;
 };
 
 __device__ __forceinline__ uint32_t align_up(uint32_t v, uint32_t a) { return (v + a - 1) & ~(a - 1); }
@@ -190,6 +192,29 @@ __device__ __forceinline__ void last_piece(float (&v)[32], uint32_t acc, uint32_
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] += w[i];
     }
+}
+
+// Eight columns' sums over the warp's rows, a lane's row in v: the lane has that of column lane / 4.
+__device__ __forceinline__ float over_rows8(const Pair (&v)[4], bool live, int lane)
+{
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 h = halves(v[i]);
+        f[2 * i] = live ? h.x : 0.f;
+        f[2 * i + 1] = live ? h.y : 0.f;
+    }
+#pragma unroll
+    for (int n = 4, o = 16; n > 0; n /= 2, o /= 2) {         // a lane keeps half of its columns and gives the others away
+        const bool upper = lane & o;
+#pragma unroll
+        for (int i = 0; i < n; ++i) {
+            const float keep = upper ? f[i + n] : f[i], give = upper ? f[i] : f[i + n];
+            f[i] = keep + __shfl_xor_sync(~0u, give, o);
+        }
+    }
+    f[0] += __shfl_xor_sync(~0u, f[0], 2);
+    return f[0] + __shfl_xor_sync(~0u, f[0], 1);
 }
 
 // One epilogue warp's state.
@@ -535,6 +560,16 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                                 }
                                 shared_store(ag, pack8<T>(gq));
                                 shared_store(au, pack8<T>(uq));
+                                if (p.sums[0]) {
+                                    const bool live = row + lane < p.m;
+                                    const float sg = over_rows8(gq, live, lane), su = over_rows8(uq, live, lane);
+                                    const int at = col + c * 64 + h * 32 + q * 8 + lane / 4;
+                                    if (lane % 4 == 0 && at < p.n) {
+                                        const int64_t to = (int64_t)(row / 32) * p.sums_ld + at;
+                                        p.sums[0][to] = sg;
+                                        p.sums[1][to] = su;
+                                    }
+                                }
                             }
                         }
                         epi_store(w, 0, &p.out[0], col + 64 * c, row);
@@ -811,6 +846,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
         const int64_t in_ld = p.in_ld[EPI == kEpiLinear ? g : 0], out_ld = p.out_ld[EPI == kEpiLinear && g ? 1 : 0];
         const int r0 = valid_rows * share / split, r1 = valid_rows * (share + 1) / split;
         const uint32_t own = smem_addr(part) + lane * 16;
+        float sum_g[2][4] = {}, sum_u[2][4] = {};             // kEpiGatedBack: over the warp's rows
         // four rows at a time: their loads are under way together
         for (int first = r0 + warp - 2; first < r1 && valid0 > 0; first += 8 * kRowsAhead) {
             float lo[kRowsAhead][4], hi[kRowsAhead][4];
@@ -870,8 +906,19 @@ split_product_kernel(const __grid_constant__ ProductParams p)
                         gate_back4(p.act, v, gv, uv);
                         row_store<TO, 4>(out0 + row * out_ld + col, valid, gv);
                         row_store<TO, 4>(out1 + row * p.out_ld[1] + col, valid, uv);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { sum_g[side][i] += gv[i]; sum_u[side][i] += uv[i]; }
                     }
                 }
+            }
+        }
+        if (EPI == kEpiGatedBack && p.sums[0]) {
+            const int64_t to = (((int64_t)tm * 2 + half) * split + share) * 8 + warp - 2;
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+                const int col = side ? col1 : col0, valid = side ? valid1 : valid0;
+                row_store<float, 4>(p.sums[0] + to * p.sums_ld + col, valid, sum_g[side]);
+                row_store<float, 4>(p.sums[1] + to * p.sums_ld + col, valid, sum_u[side]);
             }
         }
     }
@@ -1024,6 +1071,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
         }
         T *out0 = reinterpret_cast<T *>(p.out_p[0]), *out1 = reinterpret_cast<T *>(p.out_p[1]), *out2 = reinterpret_cast<T *>(p.out_p[2]);
         const T *in0 = reinterpret_cast<const T *>(p.in_p[0]), *in1 = reinterpret_cast<const T *>(p.in_p[1]);
+        float sum_g[4] = {}, sum_u[4] = {};                   // kEpiGatedBack: over the warp's tokens
         for (int64_t r = r0 + warp - 2; r < r1 && valid > 0; r += 4) {
             const uint32_t at = own + (uint32_t)r * (kFewPitch * 4);
             float lo[4] = {0.f, 0.f, 0.f, 0.f}, hi[4] = {0.f, 0.f, 0.f, 0.f};
@@ -1060,7 +1108,14 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
                 gate_back4(p.act, lo, gv, uv);
                 row_store<T, 4>(out0 + r * p.out_ld[0] + col, valid, gv);
                 row_store<T, 4>(out1 + r * p.out_ld[1] + col, valid, uv);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { sum_g[i] += gv[i]; sum_u[i] += uv[i]; }
             }
+        }
+        if (EPI == kEpiGatedBack && p.sums[0]) {
+            const int64_t to = (part_of * 4 + warp - 2) * p.sums_ld + col;
+            row_store<float, 4>(p.sums[0] + to, valid, sum_g);
+            row_store<float, 4>(p.sums[1] + to, valid, sum_u);
         }
     }
     __syncthreads();
@@ -1203,6 +1258,12 @@ ProductPlan choose_plan(const Product &p, const OperatorLaunch &l, int64_t unali
     return plan;
 }
 
+int64_t product_sum_rows(const Product &p, const ProductPlan &plan)
+{
+    if (plan.few) return 4 * plan.split;
+    return plan.pair ? ceil_div(p.m, 32) : ceil_div(p.m, 128) * plan.split * 8;
+}
+
 cudaError_t launch_product(OperatorLaunch &l, const Product &q, const ProductPlan &plan)
 {
     if (!encode_function()) return cudaErrorNotSupported;
@@ -1221,6 +1282,7 @@ cudaError_t launch_product(OperatorLaunch &l, const Product &q, const ProductPla
     p.split = plan.split;
     p.few = plan.few ? (int32_t)ceil_div(q.m, 16) * 16 : 0;
     p.status = l.status;
+    p.sums_ld = q.sums_ld;
     bool ok = true;
     for (int i = 0; i < 2; ++i) {
         p.steps[i] = (int32_t)ceil_div(q.k[i], 64);
@@ -1242,6 +1304,7 @@ cudaError_t launch_product(OperatorLaunch &l, const Product &q, const ProductPla
     for (int i = 0; i < 2; ++i) {
         p.in_p[i] = q.in[i].p;
         p.in_ld[i] = q.in[i].ld;
+        p.sums[i] = q.sums[i];
         if (plan.pair && q.in[i].p) ok = ok && encode(&p.in[i], to, eo, q.in[i], q.m, q.n, 32);
     }
     if (!ok) return cudaErrorInvalidValue;

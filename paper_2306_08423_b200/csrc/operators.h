@@ -37,6 +37,10 @@ struct Product {
     Matrix out[3];
     int in_type = 0;              // DISTSIM_BF16 or DISTSIM_F16: operands, bias, in and out
     bool wide = false;            // out and in are 32-bit floats (kEpiLinear without bias and activation)
+    // kEpiGatedBack: column sums of out0 and out1 before they are rounded (both or none), as partials:
+    // product_sum_rows() rows of n values, sums_ld (a multiple of 4) apart, which add up to them.
+    float *sums[2] = {nullptr, nullptr};
+    int64_t sums_ld = 0;
 };
 
 struct OperatorLaunch {
@@ -101,6 +105,7 @@ inline bool aligned_rows(const Matrix &x, int elem_bytes)
 }
 // Operands have aligned rows; for plan.pair so have in and out, and the 16-byte piece that holds the last
 // column of an out row is written whole.  m, n >= 1, k[0] >= 1.
+int64_t product_sum_rows(const Product &p, const ProductPlan &plan);
 cudaError_t launch_product(OperatorLaunch &l, const Product &p, const ProductPlan &plan);
 
 // Column-wise passes over [rows][cols] matrices of 16-bit types (column_kernels.cu).
@@ -112,6 +117,7 @@ struct ColumnPass {
         int64_t cols = 0;
         Matrix x;                 // in; null: no such part
         void *sums = nullptr;     // [cols] column sums (of the unrounded product), nullable with `out` only
+        int64_t partials = 0;     // > 0: x is that many rows of 32-bit partial sums instead, whole eights in aligned rows
     } part[kPassParts];           // all in one launch; with z or out one part
     Matrix z;                     // in, nullable: x is multiplied by act'(z)
     int act = 0;

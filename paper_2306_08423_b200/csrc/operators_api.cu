@@ -543,12 +543,17 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     dwd.plan(c, plan_d.pair, true);
     const int64_t ld_i = padded_ld(f, 2);
     const size_t dg_at = inner ? c.room((size_t)t * ld_i * 2) : 0, du_at = inner ? c.room((size_t)t * ld_i * 2) : 0;
-    const size_t part_at = o->db_gate || o->db_up || o->db_down
+    // db_gate and db_up: from the first product's epilogue, which has dg and du before they are rounded
+    const bool inner_sums = o->db_gate || o->db_up;
+    const int64_t sum_rows = inner_sums ? product_sum_rows(pi, plan_i) : 0, ld_sums = ceil_div(f, 8) * 8;
+    const size_t sums_at = c.room((size_t)(2 * sum_rows * ld_sums) * 4);
+    const size_t part_at = inner_sums || o->db_down
         ? c.room((size_t)column_pass_partials(2 * f + d, c.l.sm_count) * 4) : 0;
     if ((rc = c.reserve()) != DISTSIM_OK) return rc;
     for (StandIn *s : {&x, &dy, &h, &g, &u, &wg, &wu, &wd, &dx, &dwg, &dwu, &dwd}) s->place(c);
     const Matrix dg = inner ? mat(c.at(dg_at), ld_i) : Matrix{}, du = inner ? mat(c.at(du_at), ld_i) : Matrix{};
-    float *partial = part_at || o->db_gate || o->db_up || o->db_down ? c.at<float>(part_at) : nullptr;
+    float *partial = inner_sums || o->db_down ? c.at<float>(part_at) : nullptr;
+    Matrix sums[2];
 
     TRY(fetch(c, {&dy, &wd, &g, &u, &wg, &wu, &x, &h}));
     if (inner) {
@@ -558,6 +563,11 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
         pi.in[1] = u.use;
         pi.out[0] = dg;
         pi.out[1] = du;
+        for (int i = 0; i < 2 && inner_sums; ++i) {
+            pi.sums[i] = c.at<float>(sums_at) + i * sum_rows * ld_sums;
+            sums[i] = mat(pi.sums[i], ld_sums);
+        }
+        pi.sums_ld = ld_sums;
         TRY(launch_product(c.l, pi, plan_i));
     }
     if (o->dx) {
@@ -589,8 +599,8 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     }
     TRY(give_back(c, {&dx, &dwg, &dwu, &dwd}));
     ColumnPass pass = column_pass(c, o->dtype, t, o->grad_dtype, partial);
-    if (o->db_gate) pass.part[0] = {f, dg, o->db_gate};
-    if (o->db_up) pass.part[1] = {f, du, o->db_up};
+    if (o->db_gate) pass.part[0] = {f, sums[0], o->db_gate, sum_rows};
+    if (o->db_up) pass.part[1] = {f, sums[1], o->db_up, sum_rows};
     if (o->db_down) pass.part[2] = {d, dy.use, o->db_down};
     TRY(launch_column_pass(c.l, pass));
     return c.end(e);

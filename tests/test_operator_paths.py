@@ -177,3 +177,33 @@ def test_slopes_of_arguments_whose_square_is_infinite(ctx, plan, act):
     du = torch.where(z > 0, z, torch.zeros_like(z))
     E.distsim_gated_ffn_backward(ctx, torch.ones_like(z), z, eye, eye, eye, None, z, torch.ones_like(z), dx=dg, activation=act)
     assert torch.equal(dg, (up.float() + du.float()).bfloat16())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan", [0, -1, 1, 2, 4, -2, -3, -4], indirect=True)
+@pytest.mark.parametrize("shape", [(1, 64, 64, 0, 0), (7, 100, 130, 0, 0), (64, 136, 263, 1, 0), (129, 72, 520, 3, 1), (385, 64, 1030, 0, 0), (2100, 64, 96, 0, 0)])
+@pytest.mark.parametrize("act", ["silu", "none"])
+def test_gated_bias_gradients_are_summed_before_rounding(ctx, plan, shape, act):
+    """As the linear one's: what dg and du lose to bf16 on their way into the products does not reach db_gate and db_up.
+    Off by dh's sum (k 2^-23 of its magnitudes), the activation's 2^-19 and the column sum's own 2^-23 a term."""
+    from paper_2306_08423_b200 import engine as E
+    t, d, f, pad, shift = shape
+    rng = np.random.default_rng(t + f)
+    dt = torch.bfloat16
+    o = ffn_case(rng, *shape, dt)
+    dy, g, u = randn(rng, t, d, dtype=dt), *(randn(rng, t, f, dtype=dt, pad=pad, shift=shift) for _ in range(2))
+    db = {n: torch.full((k,), 7.0, device="cuda") for n, k in (("db_gate", f), ("db_up", f), ("db_down", d))}
+    dx = torch.empty(t, d, dtype=dt, device="cuda")
+    E.distsim_gated_ffn_backward(ctx, dy, **o, hidden=None, gate=g, up=u, dx=dx, activation=act, **db)
+    dh = dy.double() @ o["w_down"].double()
+    dh_off = (d + 2) * U32 * dy.double().abs() @ o["w_down"].double().abs()
+    val, slope = act64(g.double(), act)
+    approx = 2.0 ** -19 * g.double().abs().clamp_min(1) if act != "none" else 0
+    dg, du = dh * u.double() * slope, dh * val
+    for name, q, off in (("db_gate", dg, u.double().abs() * (dh_off * slope.abs() + (dh.abs() + dh_off) * approx)),
+                         ("db_up", du, dh_off * val.abs() + (dh.abs() + dh_off) * approx)):
+        close(name, db[name], q.sum(0), off.sum(0) + (t + 4) * U32 * q.abs().sum(0))
+    close("db_down", db["db_down"], dy.double().sum(0), (t + 2) * U32 * dy.double().abs().sum(0))
+    again = {n: torch.empty_like(v) for n, v in db.items()}
+    E.distsim_gated_ffn_backward(ctx, dy, **o, hidden=None, gate=g, up=u, activation=act, **again)
+    assert all(torch.equal(v, db[n]) for n, v in again.items())
