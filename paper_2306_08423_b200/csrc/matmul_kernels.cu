@@ -92,6 +92,31 @@ __device__ __forceinline__ uint32_t align_up(uint32_t v, uint32_t a) { return (v
 
 __device__ __forceinline__ void give_up(int32_t *status) { *reinterpret_cast<volatile int32_t *>(status) = DISTSIM_E_TIMEOUT; }
 
+// By a producer behind its last load (of `loads` so far): until every stage has been consumed, so that
+// nothing arrives at the block's barriers or memory once it has left.  A producer that gave up, or does so
+// here, waits as long as copies could take: some of them report to the other block's barriers.
+template <int STAGES>
+__device__ __forceinline__ bool consumed(const uint64_t (&empty)[STAGES], int loads, bool ok, int32_t *status)
+{
+    for (int i = max(0, loads - STAGES); i < loads && ok; ++i) ok = mbar_wait(smem_addr(&empty[i % STAGES]), (i / STAGES) & 1);
+    if (!ok) {
+        give_up(status);
+        for (int i = max(0, loads - STAGES); i < loads; ++i) mbar_wait(smem_addr(&empty[i % STAGES]), (i / STAGES) & 1, kDrainPolls);
+    }
+    return ok;
+}
+// By the thread that issues products, behind the last one: until all of them are done.
+__device__ __forceinline__ bool products_done(uint64_t &drain, uint16_t own, bool ok, int32_t *status)
+{
+    tensor_commit(smem_addr(&drain), own);
+    if (ok) ok = mbar_wait(smem_addr(&drain), 0);
+    if (!ok) {
+        give_up(status);
+        mbar_wait(smem_addr(&drain), 0, kDrainPolls);
+    }
+    return ok;
+}
+
 // Tile index -> (group, tile row, tile column): bands of 8 tile rows, rows fastest, so that the
 // tiles in flight at a time share both operands in L2.
 __device__ __forceinline__ void tile_coords(const ProductParams &p, int tile, int &group, int &tm, int &tn)
@@ -344,14 +369,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                 }
             }
         }
-        if (!ok) {
-            give_up(p.status);
-            // the copies in flight report to the first block's barriers: it sees them land, and
-            // the other block's memory stays until the cluster's last barrier
-            if (rank == 0)
-                for (int i = it < kPairStages ? 0 : it - kPairStages; i < it; ++i)
-                    mbar_wait(smem_addr(&sh.full[i % kPairStages]), (i / kPairStages) & 1, kDrainPolls);
-        }
+        consumed(sh.empty, it, ok, p.status);
     } else if (warp == 1 && rank == 0 && one_lane()) {
         // ---- products of both blocks ----
         const uint32_t a_block = p.a_mn ? kOperandBytes / 2 : 16, b_block = p.b_mn ? kOperandBytes / 2 : 16;
@@ -378,11 +396,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                 }
                 if (ok) tensor_commit(smem_addr(&sh.acc_full[acc]), 3);
             }
-        if (!ok) {
-            give_up(p.status);
-            tensor_commit(smem_addr(&sh.drain), 1);
-            mbar_wait(smem_addr(&sh.drain), 0, kDrainPolls);
-        }
+        products_done(sh.drain, 1, ok, p.status);
     } else if (warp >= 4) {
         // ---- epilogue ----
         const int ew = warp - 4, quad = ew & 3, half = ew >> 2;
@@ -757,13 +771,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
                 tile_load_pair(sb, mb, k, row_b, bar);
             }
         }
-        if (!ok) {
-            give_up(p.status);
-            if (half == 0)
-                for (int i = it < kSplitStages ? 0 : it - kSplitStages; i < it; ++i)
-                    mbar_wait(smem_addr(&sh.full[i % kSplitStages]), (i / kSplitStages) & 1, kDrainPolls);
-            sh.failed = 1;
-        }
+        if (!consumed(sh.empty, it, ok, p.status)) sh.failed = 1;
     } else if (warp == 1 && half == 0 && one_lane()) {
         const uint32_t a_block = p.a_mn ? kOperandBytes / 2 : 16, b_block = p.b_mn ? kOperandBytes / 2 : 16;
         const uint64_t a_next = p.a_mn ? 2048 >> 4 : 32 >> 4, b_next = p.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -786,12 +794,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
             }
             if (ok) tensor_commit(smem_addr(&sh.acc_full), pair_mask);
         }
-        if (!ok) {
-            give_up(p.status);
-            tensor_commit(smem_addr(&sh.drain), (uint16_t)(1u << crank));
-            mbar_wait(smem_addr(&sh.drain), 0, kDrainPolls);
-            sh.failed = 1;
-        }
+        if (!products_done(sh.drain, (uint16_t)(1u << crank), ok, p.status)) sh.failed = 1;
     }
     __syncwarp();
 
@@ -1000,13 +1003,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
             }
             tile_load_pair(sw + kOperandBytes, &p.a[seg], k, (int)half * p.few / 2, bar);
         }
-        if (!ok) {
-            give_up(p.status);
-            if (half == 0)
-                for (int i = it < kFewStages ? 0 : it - kFewStages; i < it; ++i)
-                    mbar_wait(smem_addr(&sh.full[i % kFewStages]), (i / kFewStages) & 1, kDrainPolls);
-            sh.failed = 1;
-        }
+        if (!consumed(sh.empty, it, ok, p.status)) sh.failed = 1;
     } else if (warp == 1 && half == 0 && one_lane()) {
         const uint32_t w_block = p.b_mn ? kOperandBytes / 2 : 16;
         const uint64_t w_next = p.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -1023,14 +1020,8 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
             for (int k = 0; k < 4; ++k, dw += w_next, dt += 32 >> 4) tensor_mma(tmem, dw, dt, p.idesc, it > 0 || k > 0);
             tensor_commit(smem_addr(&sh.empty[stage]), pair_mask);
         }
-        if (ok) {
-            tensor_commit(smem_addr(&sh.acc_full), pair_mask);
-        } else {
-            give_up(p.status);
-            tensor_commit(smem_addr(&sh.drain), (uint16_t)(1u << crank));
-            mbar_wait(smem_addr(&sh.drain), 0, kDrainPolls);
-            sh.failed = 1;
-        }
+        if (ok) tensor_commit(smem_addr(&sh.acc_full), pair_mask);
+        if (!products_done(sh.drain, (uint16_t)(1u << crank), ok, p.status)) sh.failed = 1;
     }
     __syncwarp();
 
