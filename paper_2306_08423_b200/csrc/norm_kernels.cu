@@ -85,7 +85,9 @@ struct Team {
     Scratch *scratch;
     int32_t *status;
     int exchanges = 0;
-    bool dead = false;                           // a wait gave up: no further waits
+    // A wait of this thread gave up.  It goes through the remaining rows without waiting, starting copies or
+    // sending, and in the end waits once for copies started before; the others' waits then give up, too.
+    bool dead = false;
     int lack = 0;                                // columns that this warp could hold and the row does not have
     int phase;                                   // values that the team's pieces start before its columns
     float inv_n;                                 // 1 / columns of a row
@@ -127,6 +129,8 @@ struct Team {
     // After the last exchange, by every thread of the block.
     __device__ __forceinline__ void close() const
     {
+        if (dead)                                // copies that were started before: of either phase that may be under way
+            for (int i = 0; i < 8; ++i) mbar_wait(smem_addr(&scratch->row[i >> 1]), (uint32_t)i & 1, kDrainPolls);
         __syncthreads();
         if (cluster > 1) cluster_sync();
     }
@@ -140,7 +144,7 @@ struct Team {
         if (!dead && !mbar_wait(smem_addr(bar), (uint32_t)phase & 1)) {
             dead = true;
             *reinterpret_cast<volatile int32_t *>(status) = DISTSIM_E_TIMEOUT;
-            mbar_wait(smem_addr(bar), (uint32_t)phase & 1, kDrainPolls);     // nothing stays in flight
+            mbar_wait(smem_addr(bar), (uint32_t)phase & 1, kDrainPolls);     // what was sent stays in flight no longer
         }
     }
     template <int N>
@@ -190,9 +194,9 @@ struct Team {
             sync();
         } else {
             const uint32_t bar = smem_addr(&scratch->arrived[turn]);
-            if (thread == 0) mbar_expect(bar, (uint32_t)(warps * cluster * 16 * FOURS));
+            if (thread == 0 && !dead) mbar_expect(bar, (uint32_t)(warps * cluster * 16 * FOURS));
             __syncwarp();
-            if (lane < cluster)
+            if (lane < cluster && !dead)
 #pragma unroll
                 for (int k = 0; k < FOURS; ++k)
                     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];"
