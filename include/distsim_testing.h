@@ -76,6 +76,14 @@ int distsim_testing_set_product_plan(distsim_ctx *ctx, int32_t plan);
  */
 int distsim_testing_set_operator_status(distsim_ctx *ctx, int32_t code);
 
+/*
+ * Polls (of a microsecond, 0 to 4194304, which is the library's own) of the operator kernels' waits
+ * before they give up.  0: at once, whatever they wait for, so that the ways out of the kernels and
+ * the report can be tested.  A kernel that has given up waits for its copies and products in flight with
+ * a limit of its own.
+ */
+int distsim_testing_set_operator_wait_polls(distsim_ctx *ctx, int32_t polls);
+
 #ifdef __cplusplus
 }
 #endif

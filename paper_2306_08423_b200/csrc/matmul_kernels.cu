@@ -78,6 +78,7 @@ struct alignas(64) ProductParams {
     int32_t has_in, has_out1;
     const void *bias[2];
     int32_t *status;
+    int32_t polls;                               // of a wait, before it gives up
     // split kernel only: pairs that share a tile, plain pointers
     int32_t split;
     int32_t few;                                 // few-rows kernel: columns the tokens take, 16 to 64
@@ -96,22 +97,22 @@ __device__ __forceinline__ void give_up(int32_t *status) { *reinterpret_cast<vol
 // nothing arrives at the block's barriers or memory once it has left.  A producer that gave up, or does so
 // here, waits as long as copies could take: some of them report to the other block's barriers.
 template <int STAGES>
-__device__ __forceinline__ bool consumed(const uint64_t (&empty)[STAGES], int loads, bool ok, int32_t *status)
+__device__ __forceinline__ bool consumed(const uint64_t (&empty)[STAGES], int loads, bool ok, const ProductParams &p)
 {
-    for (int i = max(0, loads - STAGES); i < loads && ok; ++i) ok = mbar_wait(smem_addr(&empty[i % STAGES]), (i / STAGES) & 1);
+    for (int i = max(0, loads - STAGES); i < loads && ok; ++i) ok = mbar_wait(smem_addr(&empty[i % STAGES]), (i / STAGES) & 1, p.polls);
     if (!ok) {
-        give_up(status);
+        give_up(p.status);
         for (int i = max(0, loads - STAGES); i < loads; ++i) mbar_wait(smem_addr(&empty[i % STAGES]), (i / STAGES) & 1, kDrainPolls);
     }
     return ok;
 }
 // By the thread that issues products, behind the last one: until all of them are done.
-__device__ __forceinline__ bool products_done(uint64_t &drain, uint16_t own, bool ok, int32_t *status)
+__device__ __forceinline__ bool products_done(uint64_t &drain, uint16_t own, bool ok, const ProductParams &p)
 {
     tensor_commit(smem_addr(&drain), own);
-    if (ok) ok = mbar_wait(smem_addr(&drain), 0);
+    if (ok) ok = mbar_wait(smem_addr(&drain), 0, p.polls);
     if (!ok) {
-        give_up(status);
+        give_up(p.status);
         mbar_wait(smem_addr(&drain), 0, kDrainPolls);
     }
     return ok;
@@ -259,9 +260,9 @@ __device__ __forceinline__ void epi_fetch(const EpiWarp &w, int i, const CUtenso
         tile_load(w.buf[i], map, x, y, w.bar[i]);
     }
 }
-__device__ __forceinline__ bool epi_wait(EpiWarp &w, int i)
+__device__ __forceinline__ bool epi_wait(EpiWarp &w, int i, int polls)
 {
-    const bool ok = mbar_wait(w.bar[i], w.phase[i]);
+    const bool ok = mbar_wait(w.bar[i], w.phase[i], polls);
     w.phase[i] ^= 1;
     return __all_sync(~0u, ok);
 }
@@ -346,7 +347,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
             const int row_a = tm * 256 + (int)rank * 128;
             for (int s = 0; s < steps; ++s, ++it) {
                 const int stage = it % kPairStages;
-                if (it >= kPairStages && !mbar_wait(smem_addr(&sh.empty[stage]), (it / kPairStages - 1) & 1)) { ok = false; break; }
+                if (it >= kPairStages && !mbar_wait(smem_addr(&sh.empty[stage]), (it / kPairStages - 1) & 1, p.polls)) { ok = false; break; }
                 const int seg = s >= p.steps[0];
                 const int k = (s - (seg ? p.steps[0] : 0)) * 64;
                 const CUtensorMap *ma = &p.a[p.groups == 2 ? g : seg];
@@ -369,7 +370,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                 }
             }
         }
-        consumed(sh.empty, it, ok, p.status);
+        consumed(sh.empty, it, ok, p);
     } else if (warp == 1 && rank == 0 && one_lane()) {
         // ---- products of both blocks ----
         const uint32_t a_block = p.a_mn ? kOperandBytes / 2 : 16, b_block = p.b_mn ? kOperandBytes / 2 : 16;
@@ -380,13 +381,13 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
             for (int piece = 0; piece < pieces && ok; ++piece, ++n_acc) {
                 // one accumulator with pieces (the other half holds the running sum), else two in turn
                 const int acc = pieces > 1 ? 0 : n_acc & 1, use = pieces > 1 ? n_acc : n_acc >> 1;
-                if (use > 0 && !mbar_wait(smem_addr(&sh.acc_empty[acc]), (use - 1) & 1)) { ok = false; break; }
+                if (use > 0 && !mbar_wait(smem_addr(&sh.acc_empty[acc]), (use - 1) & 1, p.polls)) { ok = false; break; }
                 tensor_fence_after();
                 const uint32_t d = tmem + acc * 256;
                 const int first = WIDE ? piece * kPieceSteps : 0, last = WIDE ? min(steps, first + kPieceSteps) : steps;
                 for (int s = first; s < last; ++s, ++it) {
                     const int stage = it % kPairStages;
-                    if (!mbar_wait(smem_addr(&sh.full[stage]), (it / kPairStages) & 1)) { ok = false; break; }
+                    if (!mbar_wait(smem_addr(&sh.full[stage]), (it / kPairStages) & 1, p.polls)) { ok = false; break; }
                     tensor_fence_after();
                     const uint32_t sa = base + stage * kStageBytes;
                     uint64_t da = tile_descriptor(sa, a_block), db = tile_descriptor(sa + kOperandBytes, b_block);
@@ -396,7 +397,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                 }
                 if (ok) tensor_commit(smem_addr(&sh.acc_full[acc]), 3);
             }
-        products_done(sh.drain, 1, ok, p.status);
+        products_done(sh.drain, 1, ok, p);
     } else if (warp >= 4) {
         // ---- epilogue ----
         const int ew = warp - 4, quad = ew & 3, half = ew >> 2;
@@ -442,7 +443,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
             __syncwarp();
             const uint32_t running = tmem + 256 + lanes + half * 128;
             for (int piece = 0; WIDE && piece < pieces - 1 && ok; ++piece, ++n_acc) {
-                if (!(ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full[0]), n_acc & 1)))) break;
+                if (!(ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full[0]), n_acc & 1, p.polls)))) break;
                 tensor_fence_after();
                 keep_piece(d + half * 128, running, piece == 0);
                 tensor_fence_before();
@@ -450,7 +451,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                 if (lane == 0) mbar_arrive_cluster(empty0);
             }
             if (!ok) break;
-            ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full[acc]), (pieces > 1 ? n_acc : n_acc >> 1) & 1));
+            ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full[acc]), (pieces > 1 ? n_acc : n_acc >> 1) & 1, p.polls));
             if (!ok) break;
             tensor_fence_after();
 
@@ -463,7 +464,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                                 if (p.has_in) { epi_fetch(w, 0, &p.in[g], col + 64, row); epi_fetch(w, 1, &p.in[g], col + 96, row); }
                             }
                             for (int h = 0; h < 2; ++h) {
-                                if (p.has_in && !(ok = epi_wait(w, h))) break;
+                                if (p.has_in && !(ok = epi_wait(w, h, p.polls))) break;
                                 float v[32];
                                 last_piece(v, d + half * 128 + c * 64 + h * 32, running + c * 64 + h * 32, pieces == 1);
 #pragma unroll
@@ -482,7 +483,7 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                             // replace it; the pre-activation then follows from the accumulators once more
                             const int at = p.has_in ? c : 0;
                             const bool both_out = p.has_out1 && !p.has_in;
-                            if (p.has_in && !(ok = epi_wait(w, c))) break;
+                            if (p.has_in && !(ok = epi_wait(w, c, p.polls))) break;
                             if (c > 0 && !p.has_in) epi_reclaim(w);
                             for (int h = 0; h < 2; ++h) {
                                 Pair v[16];
@@ -552,8 +553,8 @@ pair_product_kernel(const __grid_constant__ ProductParams p)
                             epi_fetch(w, 0, &p.in[0], col + 64, row);
                             epi_fetch(w, 1, &p.in[1], col + 64, row);
                         }
-                        ok = epi_wait(w, 0);
-                        ok = epi_wait(w, 1) && ok;
+                        ok = epi_wait(w, 0, p.polls);
+                        ok = epi_wait(w, 1, p.polls) && ok;
                         if (!ok) break;
                         for (int h = 0; h < 2; ++h) {
                             Pair v[16];
@@ -747,7 +748,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
         int it = 0;
         for (int s = s0; s < s1; ++s, ++it) {
             const int stage = it % kSplitStages;
-            if (it >= kSplitStages && !mbar_wait(smem_addr(&sh.empty[stage]), (it / kSplitStages - 1) & 1)) { ok = false; break; }
+            if (it >= kSplitStages && !mbar_wait(smem_addr(&sh.empty[stage]), (it / kSplitStages - 1) & 1, p.polls)) { ok = false; break; }
             const int seg = s >= p.steps[0];
             const int k = (s - (seg ? p.steps[0] : 0)) * 64;
             const CUtensorMap *ma = &p.a[p.groups == 2 ? g : seg];
@@ -771,7 +772,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
                 tile_load_pair(sb, mb, k, row_b, bar);
             }
         }
-        if (!consumed(sh.empty, it, ok, p.status)) sh.failed = 1;
+        if (!consumed(sh.empty, it, ok, p)) sh.failed = 1;
     } else if (warp == 1 && half == 0 && one_lane()) {
         const uint32_t a_block = p.a_mn ? kOperandBytes / 2 : 16, b_block = p.b_mn ? kOperandBytes / 2 : 16;
         const uint64_t a_next = p.a_mn ? 2048 >> 4 : 32 >> 4, b_next = p.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -779,12 +780,12 @@ split_product_kernel(const __grid_constant__ ProductParams p)
         bool ok = true;
         int it = 0;
         for (int piece = 0; piece < pieces && ok; ++piece) {
-            if (piece > 0 && !mbar_wait(smem_addr(&sh.acc_empty), (piece - 1) & 1)) { ok = false; break; }
+            if (piece > 0 && !mbar_wait(smem_addr(&sh.acc_empty), (piece - 1) & 1, p.polls)) { ok = false; break; }
             tensor_fence_after();
             const int first = s0 + (WIDE ? piece * kPieceSteps : 0), last = WIDE ? min(s1, first + kPieceSteps) : s1;
             for (int s = first; s < last; ++s, ++it) {
                 const int stage = it % kSplitStages;
-                if (!mbar_wait(smem_addr(&sh.full[stage]), (it / kSplitStages) & 1)) { ok = false; break; }
+                if (!mbar_wait(smem_addr(&sh.full[stage]), (it / kSplitStages) & 1, p.polls)) { ok = false; break; }
                 tensor_fence_after();
                 const uint32_t sa = base + stage * kStageBytes;
                 uint64_t da = tile_descriptor(sa, a_block), db = tile_descriptor(sa + kOperandBytes, b_block);
@@ -794,7 +795,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
             }
             if (ok) tensor_commit(smem_addr(&sh.acc_full), pair_mask);
         }
-        if (!products_done(sh.drain, (uint16_t)(1u << crank), ok, p.status)) sh.failed = 1;
+        if (!products_done(sh.drain, (uint16_t)(1u << crank), ok, p)) sh.failed = 1;
     }
     __syncwarp();
 
@@ -805,7 +806,7 @@ split_product_kernel(const __grid_constant__ ProductParams p)
         const uint32_t acc = tmem + ((uint32_t)(quad * 32) << 16) + side * 128, running = acc + 256;
         bool ok = true;
         for (int piece = 0; piece < pieces && ok; ++piece) {
-            ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full), piece & 1));
+            ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full), piece & 1, p.polls));
             tensor_fence_after();
             if (!ok || piece == pieces - 1) break;
             keep_piece(acc, running, piece == 0);
@@ -988,7 +989,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
         int it = 0;
         for (int s = s0; s < s1; ++s, ++it) {
             const int stage = it % kFewStages;
-            if (it >= kFewStages && !mbar_wait(smem_addr(&sh.empty[stage]), (it / kFewStages - 1) & 1)) { ok = false; break; }
+            if (it >= kFewStages && !mbar_wait(smem_addr(&sh.empty[stage]), (it / kFewStages - 1) & 1, p.polls)) { ok = false; break; }
             const int seg = s >= p.steps[0];
             const int k = (s - (seg ? p.steps[0] : 0)) * 64;
             const CUtensorMap *mw = &p.b[EPI == kEpiGated ? (int)half : seg];
@@ -1003,7 +1004,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
             }
             tile_load_pair(sw + kOperandBytes, &p.a[seg], k, (int)half * p.few / 2, bar);
         }
-        if (!consumed(sh.empty, it, ok, p.status)) sh.failed = 1;
+        if (!consumed(sh.empty, it, ok, p)) sh.failed = 1;
     } else if (warp == 1 && half == 0 && one_lane()) {
         const uint32_t w_block = p.b_mn ? kOperandBytes / 2 : 16;
         const uint64_t w_next = p.b_mn ? 2048 >> 4 : 32 >> 4;
@@ -1012,7 +1013,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
         int it = 0;
         for (int s = s0; s < s1; ++s, ++it) {
             const int stage = it % kFewStages;
-            if (!mbar_wait(smem_addr(&sh.full[stage]), (it / kFewStages) & 1)) { ok = false; break; }
+            if (!mbar_wait(smem_addr(&sh.full[stage]), (it / kFewStages) & 1, p.polls)) { ok = false; break; }
             tensor_fence_after();
             const uint32_t sw = base + stage * kFewStageBytes;
             uint64_t dw = tile_descriptor(sw, w_block), dt = tile_descriptor(sw + kOperandBytes, 16);
@@ -1021,7 +1022,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
             tensor_commit(smem_addr(&sh.empty[stage]), pair_mask);
         }
         if (ok) tensor_commit(smem_addr(&sh.acc_full), pair_mask);
-        if (!products_done(sh.drain, (uint16_t)(1u << crank), ok, p.status)) sh.failed = 1;
+        if (!products_done(sh.drain, (uint16_t)(1u << crank), ok, p)) sh.failed = 1;
     }
     __syncwarp();
 
@@ -1029,7 +1030,7 @@ few_rows_kernel(const __grid_constant__ ProductParams p)
     float *part = reinterpret_cast<float *>(ring);
     if (warp >= 2) {
         const int quad = warp & 3;
-        const bool ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full), 0));
+        const bool ok = __all_sync(~0u, mbar_wait(smem_addr(&sh.acc_full), 0, p.polls));
         tensor_fence_after();
         if (!ok) {
             if (lane == 0) { give_up(p.status); sh.failed = 1; }
@@ -1273,6 +1274,7 @@ cudaError_t launch_product(OperatorLaunch &l, const Product &q, const ProductPla
     p.split = plan.split;
     p.few = plan.few ? (int32_t)ceil_div(q.m, 16) * 16 : 0;
     p.status = l.status;
+    p.polls = l.polls;
     p.sums_ld = q.sums_ld;
     bool ok = true;
     for (int i = 0; i < 2; ++i) {

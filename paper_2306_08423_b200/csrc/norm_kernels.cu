@@ -60,6 +60,7 @@ struct NormParams {
     uint32_t ref_start, ref_pitch, ref_shift;    // addresses of the rows that phases follow (low words); log2 of a value's bytes
     float *partial;
     int32_t *status;
+    int32_t polls;                               // of a wait, before it gives up
     bool sum_q, sum_qx, sum_y;                   // which column sums are wanted: S0; S1; S2 and S3
     int32_t slot[4];                             // place of S0..S3 among the kept sums (-1: not kept)
     int32_t n_sums;
@@ -83,7 +84,7 @@ struct Team {
     int id, thread, threads, cluster;
     uint32_t rank;
     Scratch *scratch;
-    int32_t *status;
+    int32_t *status, polls;
     int exchanges = 0;
     // A wait of this thread gave up.  It goes through the remaining rows without waiting, starting copies or
     // sending, and in the end waits once for copies started before; the others' waits then give up, too.
@@ -103,6 +104,7 @@ struct Team {
         rank = p.cluster > 1 ? cluster_rank() : 0;
         scratch = all + id;
         status = p.status;
+        polls = p.polls;
         inv_n = 1.f / (float)p.cols;
         phase = (int)(((p.ref_start + (uint32_t)((blockIdx.x / p.cluster) * p.teams + id) * p.ref_pitch) & 15) >> p.ref_shift);
         if (thread == 0) {
@@ -141,7 +143,7 @@ struct Team {
     }
     __device__ __forceinline__ void wait(uint64_t *bar, int phase)
     {
-        if (!dead && !mbar_wait(smem_addr(bar), (uint32_t)phase & 1)) {
+        if (!dead && !mbar_wait(smem_addr(bar), (uint32_t)phase & 1, polls)) {
             dead = true;
             *reinterpret_cast<volatile int32_t *>(status) = DISTSIM_E_TIMEOUT;
             mbar_wait(smem_addr(bar), (uint32_t)phase & 1, kDrainPolls);     // what was sent stays in flight no longer
@@ -1195,6 +1197,7 @@ cudaError_t launch_residual_norm_forward(OperatorLaunch &l, const ResidualNorm &
 {
     NormParams p = base_params(r);
     p.status = l.status;
+    p.polls = l.polls;
     switch (r.type) {
     case DISTSIM_F32: return forward<float>(l, p);
     case DISTSIM_F16: return forward<__half>(l, p);
@@ -1223,6 +1226,7 @@ cudaError_t launch_residual_norm_backward(OperatorLaunch &l, const ResidualNorm 
     NormParams p = base_params(r);
     p.partial = r.partial;
     p.status = l.status;
+    p.polls = l.polls;
     p.sum_q = r.dpost_bias || (r.dgate && r.post_weight && r.post_bias);
     p.sum_qx = r.dpost_weight || r.dgate;
     p.sum_y = r.dweight || r.dbias;

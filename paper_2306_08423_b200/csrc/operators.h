@@ -8,6 +8,10 @@
 
 namespace distsim {
 
+// Polls of an operator kernel's wait, of a microsecond each: it gives up after some seconds at most; the
+// longest wait of a healthy launch (an accumulator's whole product) takes microseconds.
+constexpr int32_t kOperatorPolls = 1 << 22;
+
 // A matrix of `rows` rows, `ld` elements apart, whose columns are contiguous.
 struct Matrix {
     const void *p = nullptr;
@@ -48,6 +52,7 @@ struct OperatorLaunch {
     int sm_count = 0;
     const int *split_capacity = nullptr;         // of the device, for splits of 1, 2, 4
     int32_t *status = nullptr;    // host-mapped word that a kernel whose wait gave up writes
+    int32_t polls = kOperatorPolls;
     int64_t launches = 0;
 };
 

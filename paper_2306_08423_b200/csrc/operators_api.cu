@@ -26,7 +26,7 @@ struct OperatorState {
     Retired *retired = nullptr;                  // earlier blocks that graphs may still hold
     int sm_count = 0;
     int split_capacity[3] = {};                  // of the context's device, see operators.h
-    int32_t forced_plan = 0;                     // testing hook, see distsim_testing.h
+    int32_t forced_plan = 0, polls = kOperatorPolls;         // testing hooks, see distsim_testing.h
     bool ready = false;
 
     ~OperatorState()
@@ -106,6 +106,7 @@ struct Call {
         l.sm_count = s.sm_count;
         l.split_capacity = s.split_capacity;
         l.status = s.d_status;
+        l.polls = s.polls;
         return DISTSIM_OK;
     }
     int take_status()
@@ -315,6 +316,15 @@ int distsim_testing_set_operator_status(distsim_ctx *ctx, int32_t code)
     Call c(ctx, nullptr);
     const int rc = c.begin();
     if (rc == DISTSIM_OK) *reinterpret_cast<volatile int32_t *>(c.a.state->status) = code;
+    return rc;
+}
+
+int distsim_testing_set_operator_wait_polls(distsim_ctx *ctx, int32_t polls)
+{
+    if (!ctx || polls < 0 || polls > kOperatorPolls) return DISTSIM_E_ARG;
+    Call c(ctx, nullptr);
+    const int rc = c.begin();
+    if (rc == DISTSIM_OK) c.a.state->polls = polls;
     return rc;
 }
 

@@ -9,10 +9,8 @@
 
 namespace distsim {
 
-// Polls of one wait, each of which may sleep for kPollNs: a wait gives up after some seconds at
-// most; the longest wait of a healthy launch (an accumulator's whole product) takes microseconds.
-// Without the hint of how long to sleep, waiting warps took a third of the issue slots.
-constexpr int kOperatorPolls = 1 << 22;
+// Each poll of a wait may sleep for kPollNs.  Without the hint of how long to sleep, waiting warps took a
+// third of the issue slots.
 constexpr uint32_t kPollNs = 1000;
 
 __device__ __forceinline__ bool one_lane()
@@ -44,7 +42,7 @@ __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar)
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(cluster_bar) : "memory");
 }
 // Waits for the phase of the given parity, at most `polls` polls.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int polls = kOperatorPolls)
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int polls)
 {
     for (int i = 0; i < polls; ++i) {
         uint32_t done;

@@ -32,7 +32,8 @@ TESTING_EXPORTS = ("distsim_testing_set_stage_wait_polls", "distsim_testing_laun
                    "distsim_testing_space_cells", "distsim_testing_lockstep_pieces",
                    "distsim_testing_bidirectional_order",
                    "distsim_testing_time_phases", "distsim_testing_last_phase_ms",
-                   "distsim_testing_set_product_plan", "distsim_testing_set_operator_status")
+                   "distsim_testing_set_product_plan", "distsim_testing_set_operator_status",
+                   "distsim_testing_set_operator_wait_polls")
 TOPK_STATIC_MAX_K = 1024
 
 
@@ -78,6 +79,7 @@ _lib.distsim_testing_time_phases.argtypes = [C.c_void_p, C.c_int32]
 _lib.distsim_testing_last_phase_ms.argtypes = [C.c_void_p, C.POINTER(C.c_float), C.POINTER(C.c_float)]
 _lib.distsim_testing_set_product_plan.argtypes = [C.c_void_p, C.c_int32]
 _lib.distsim_testing_set_operator_status.argtypes = [C.c_void_p, C.c_int32]
+_lib.distsim_testing_set_operator_wait_polls.argtypes = [C.c_void_p, C.c_int32]
 _lib.distsim_load_event_table.argtypes = [C.c_void_p, C.POINTER(_Table)]
 _lib.distsim_set_space.argtypes = [C.c_void_p, C.POINTER(_Space), C.POINTER(C.c_int64)]
 _lib.distsim_decode.argtypes = [C.c_void_p, C.c_int64, C.POINTER(_Candidate)]
@@ -436,3 +438,8 @@ def distsim_testing_set_product_plan(ctx: Context, plan: int) -> None:
 def distsim_testing_set_operator_status(ctx: Context, code: int) -> None:
     """Sets the word an operator kernel whose wait gave up would set."""
     ctx._check(_lib.distsim_testing_set_operator_status(ctx._h, code))
+
+
+def distsim_testing_set_operator_wait_polls(ctx: Context, polls: int) -> None:
+    """Polls of the operator kernels' waits before they give up (0: at once; the library's default is 4194304)."""
+    ctx._check(_lib.distsim_testing_set_operator_wait_polls(ctx._h, polls))

@@ -647,3 +647,91 @@ def test_norm_gradients_one_by_one(ctx, dtype, shape, parts):
                 assert torch.equal(v, whole[k]), (wanted, k)
             else:
                 near((wanted, k), v, whole[k].double(), 64 * 2.0 ** -24 + (2.0 ** -10 if dtype != torch.float32 else 0))
+
+
+# ---------------------------------------------------------------- waits that give up
+
+@pytest.fixture
+def impatient():
+    """A context of its own, and what makes the operators' waits give up at once while it runs."""
+    from paper_2306_08423_b200 import engine as E
+    c = E.Context(0)
+
+    def gives_up(call):
+        E.distsim_testing_set_operator_wait_polls(c, 0)
+        call()
+        with pytest.raises(E.DistsimError) as e:
+            E.distsim_operator_status(c)
+        assert e.value.code == E.E_TIMEOUT
+        E.distsim_testing_set_operator_wait_polls(c, 1 << 22)
+        E.distsim_operator_status(c)                 # reported once
+    yield c, gives_up
+    E.distsim_testing_set_product_plan(c, 0)
+    E.distsim_operator_status(c)
+    c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan_of", [-1, 1, 4, -2, -4])
+@pytest.mark.parametrize("d", [64, 648])             # fewer steps than a ring has stages, and more
+def test_products_that_give_up(impatient, plan_of, d):
+    """Every wait of the product kernels gives up at once: the kernels end, say so, and leave nothing behind that the next
+    call would meet."""
+    from paper_2306_08423_b200 import engine as E
+    c, gives_up = impatient
+    E.distsim_testing_set_product_plan(c, plan_of)
+    t, f = 60, 520
+    rng = np.random.default_rng(d)
+    dt = torch.bfloat16
+    x, w, b, r = linear_case(rng, t, d, f, 0, 0, dt)
+    y, z = torch.empty(t, f, dtype=dt, device="cuda"), torch.empty(t, f, dtype=dt, device="cuda")
+    o = ffn_case(rng, t, d, f, 0, 0, dt)
+    g, u = torch.empty_like(y), torch.empty_like(y)
+    yd, dx, dw = torch.empty(t, d, dtype=dt, device="cuda"), torch.empty(t, d, dtype=dt, device="cuda"), torch.empty(f, d, device="cuda")
+    many = randn(rng, 1100, d, dtype=dt), randn(rng, 1100, f, dtype=dt)
+    calls = [(lambda: E.distsim_linear_forward(c, x, w, y, bias=b, residual=r, preact=z, activation="gelu"), (y, z)),
+             (lambda: E.distsim_gated_ffn_forward(c, **o, y=yd, hidden=y, gate=g, up=u), (yd, y, g, u)),
+             (lambda: E.distsim_gated_ffn_backward(c, yd, **o, hidden=None, gate=r, up=z, dx=dx), (dx,))]
+    if plan_of > -2:                                 # in pieces
+        calls.append((lambda: E.distsim_linear_backward(c, many[1], many[0], w, dweight=dw, dweight_in=dw), (dw,)))
+    for call, out in calls:
+        for v in out:
+            v.fill_(1.0)
+        call()
+        first = [v.clone() for v in out]
+        gives_up(call)
+        for v in out:
+            v.fill_(1.0)
+        call()
+        E.distsim_operator_status(c)
+        assert all(torch.equal(a, v) for a, v in zip(first, out))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(9, 256, 0, 0), (700, 768, 0, 0), (33, 1000, 1, 3), (5, 2047, 0, 1), (7, 5000, 0, 0), (40, 12288, 0, 0), (3, 16381, 0, 1)])
+@pytest.mark.parametrize("parts", [(1, 1, 1, 1, 1, 0.1), (0, 0, 0, 1, 0, 0.0)])
+def test_norms_that_give_up(impatient, shape, parts):
+    from paper_2306_08423_b200 import engine as E
+    c, gives_up = impatient
+    t, n, pad, shift = shape
+    post, pre = parts[:2]
+    dt = torch.bfloat16
+    rng = np.random.default_rng(n)
+    x, r, o, bias = norm_case(rng, shape, parts, dt)
+    h, dy, dh = (randn(rng, t, n, dtype=dt, pad=pad, shift=shift) for _ in range(3))
+    out = [torch.empty(t, n, dtype=dt, device="cuda") for _ in range(4)]
+    names = [k for k, v in (("dgate", parts[2]), ("dpost_weight", post), ("dpost_bias", post), ("dweight", pre), ("dbias", pre)) if v]
+    grads = {k: torch.empty(n, dtype=dt, device="cuda") for k in names}
+    kw = dict(kind="layer", alpha=0.75, p=parts[5], seed=5, offset=9)
+    calls = [(lambda: E.distsim_residual_norm_forward(c, x, residual=r, h=out[0], y=out[1] if pre else None, bias=bias, **o, **kw), out[:1 + pre]),
+             (lambda: E.distsim_residual_norm_backward(c, x, h if pre else None, dy=dy if pre else None, dh=dh, dx=out[2], dresidual=out[3],
+                                                       **grads, **o, **kw), out[2:] + list(grads.values()))]
+    for call, got in calls:
+        call()
+        first = [v.clone() for v in got]
+        gives_up(call)
+        for v in got:
+            v.fill_(7.0)
+        call()
+        E.distsim_operator_status(c)
+        assert all(torch.equal(a, v) for a, v in zip(first, got))
