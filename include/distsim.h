@@ -436,12 +436,13 @@ int distsim_linear_backward(distsim_ctx *ctx, void *stream, const distsim_linear
  *   forward    g = x w_gate^T + b_gate;  u = x w_up^T + b_up;  h = activation(g) * u   (one kernel)
  *              y = h w_down^T + b_down + residual
  *   backward   dh = dy w_down;  dg = dh * u * activation'(g);  du = dh * activation(g)  (one kernel)
- *              dx = dg w_gate + du w_up;  dw_gate = dg^T x;  dw_up = du^T x;  dw_down = dy^T h;
+ *              dx = dg w_gate + du w_up;  dw_gate = dw_gate_in + dg^T x;  dw_up = dw_up_in + du^T x;
+ *              dw_down = dw_down_in + dy^T h;
  *              db_gate, db_up, db_down = sums of dg, du, dy over the tokens
  * h, dg and du are rounded to dtype (they are operands of the next products); db_gate and db_up are
  * summed before that.
  * Nullable: the biases, residual; forward: hidden, gate, up (gate and up together); backward: any
- * gradient.  dtype: DISTSIM_BF16 or DISTSIM_F16.
+ * gradient, and each dw_*_in.  dtype: DISTSIM_BF16 or DISTSIM_F16.
  */
 typedef struct {
     int64_t tokens, d_in, d_hidden;
@@ -455,6 +456,8 @@ typedef struct {
     void *dx, *dw_gate, *dw_up, *dw_down, *db_gate, *db_up, *db_down;
     int64_t ld_x, ld_w_gate, ld_w_up, ld_w_down, ld_residual, ld_y, ld_hidden, ld_gate, ld_up;
     int64_t ld_dy, ld_dx, ld_dw_gate, ld_dw_up, ld_dw_down;
+    const void *dw_gate_in, *dw_up_in, *dw_down_in;   /* gradients of earlier micro-batches, of grad_dtype; */
+    int64_t ld_dw_gate_in, ld_dw_up_in, ld_dw_down_in; /* may be dw_gate, dw_up, dw_down themselves         */
 } distsim_gated_ffn;
 
 int distsim_gated_ffn_forward(distsim_ctx *ctx, void *stream, const distsim_gated_ffn *h_op);

@@ -143,7 +143,7 @@ struct Move {
     const uint16_t *src;
     int64_t ld_dst, ld_src, rows, cols;
 };
-constexpr int kMostMoves = 8;
+constexpr int kMostMoves = 11;
 cudaError_t launch_moves(OperatorLaunch &l, const Move *moves, int n);
 
 // The residual connection (norm_kernels.cu).

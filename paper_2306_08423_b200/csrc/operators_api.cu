@@ -449,7 +449,8 @@ int check_ffn(Call &c, const distsim_gated_ffn *o)
         bad_rows(o->w_down, o->ld_w_down, f) || bad_rows(o->residual, o->ld_residual, d) || bad_rows(o->y, o->ld_y, d) ||
         bad_rows(o->hidden, o->ld_hidden, f) || bad_rows(o->gate, o->ld_gate, f) || bad_rows(o->up, o->ld_up, f) ||
         bad_rows(o->dy, o->ld_dy, d) || bad_rows(o->dx, o->ld_dx, d) || bad_rows(o->dw_gate, o->ld_dw_gate, d) ||
-        bad_rows(o->dw_up, o->ld_dw_up, d) || bad_rows(o->dw_down, o->ld_dw_down, f))
+        bad_rows(o->dw_up, o->ld_dw_up, d) || bad_rows(o->dw_down, o->ld_dw_down, f) || bad_rows(o->dw_gate_in, o->ld_dw_gate_in, d) ||
+        bad_rows(o->dw_up_in, o->ld_dw_up_in, d) || bad_rows(o->dw_down_in, o->ld_dw_down_in, f))
         return c.fail(DISTSIM_E_ARG, "gated ffn: rows closer together than they are long");
     return DISTSIM_OK;
 }
@@ -515,12 +516,15 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     cudaError_t e = cudaSuccess;
     if (t == 0) {
         if ((rc = c.reserve()) != DISTSIM_OK) return rc;
-        Move zeros[3];
+        Move whole[3];
         int n = 0;
-        if (o->dw_gate) zeros[n++] = move_of(mat(o->dw_gate, o->ld_dw_gate), Matrix{}, f, d, ge);
-        if (o->dw_up) zeros[n++] = move_of(mat(o->dw_up, o->ld_dw_up), Matrix{}, f, d, ge);
-        if (o->dw_down) zeros[n++] = move_of(mat(o->dw_down, o->ld_dw_down), Matrix{}, d, f, ge);
-        TRY(launch_moves(c.l, zeros, n));
+        const auto take = [&](const Matrix &dw, const Matrix &in, int64_t rows, int64_t cols) {
+            if (dw.p && dw.p != in.p) whole[n++] = move_of(dw, in, rows, cols, ge);
+        };
+        take(mat(o->dw_gate, o->ld_dw_gate), mat(o->dw_gate_in, o->ld_dw_gate_in), f, d);
+        take(mat(o->dw_up, o->ld_dw_up), mat(o->dw_up_in, o->ld_dw_up_in), f, d);
+        take(mat(o->dw_down, o->ld_dw_down), mat(o->dw_down_in, o->ld_dw_down_in), d, f);
+        TRY(launch_moves(c.l, whole, n));
         TRY(zero_vector(c, o->db_gate, f, o->grad_dtype));
         TRY(zero_vector(c, o->db_up, f, o->grad_dtype));
         TRY(zero_vector(c, o->db_down, d, o->grad_dtype));
@@ -534,14 +538,17 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     pi.m = t; pi.n = f; pi.k[0] = d; pi.b_mn = true; pi.epilogue = kEpiGatedBack; pi.act = o->activation; pi.in_type = o->dtype;
     px.m = t; px.n = d; px.k[0] = px.k[1] = f; px.b_mn = true; px.in_type = o->dtype;
     pw.m = f; pw.n = d; pw.k[0] = t; pw.a_mn = pw.b_mn = true; pw.in_type = o->dtype; pw.wide = ge == 4;
-    pw.groups = o->dw_gate && o->dw_up ? 2 : 1;
+    const bool two = o->dw_gate && o->dw_up;
+    pw.groups = two && !o->dw_gate_in == !o->dw_up_in ? 2 : 1;            // in one launch, unless one alone is added to
     pd.m = d; pd.n = f; pd.k[0] = t; pd.a_mn = pd.b_mn = true; pd.in_type = o->dtype; pd.wide = ge == 4;
     StandIn x = stand_in(o->x, o->ld_x, t, d, 2), dy = stand_in(o->dy, o->ld_dy, t, d, 2), h = stand_in(o->hidden, o->ld_hidden, t, f, 2);
     StandIn g = stand_in(o->gate, o->ld_gate, t, f, 2), u = stand_in(o->up, o->ld_up, t, f, 2);
     StandIn wg = stand_in(o->w_gate, o->ld_w_gate, f, d, 2), wu = stand_in(o->w_up, o->ld_w_up, f, d, 2), wd = stand_in(o->w_down, o->ld_w_down, d, f, 2);
     StandIn dx = stand_in(o->dx, o->ld_dx, t, d, 2), dwg = stand_in(o->dw_gate, o->ld_dw_gate, f, d, ge), dwu = stand_in(o->dw_up, o->ld_dw_up, f, d, ge);
-    StandIn dwd = stand_in(o->dw_down, o->ld_dw_down, d, f, ge);
-    const ProductPlan plan_i = c.plan(pi, {&g, &u}, {}), plan_x = c.plan(px, {}, {&dx}), plan_w = c.plan(pw, {}, {&dwg, &dwu}), plan_d = c.plan(pd, {}, {&dwd});
+    StandIn dwd = stand_in(o->dw_down, o->ld_dw_down, d, f, ge), dwgi = stand_in(o->dw_gate ? o->dw_gate_in : nullptr, o->ld_dw_gate_in, f, d, ge);
+    StandIn dwui = stand_in(o->dw_up ? o->dw_up_in : nullptr, o->ld_dw_up_in, f, d, ge), dwdi = stand_in(o->dw_down ? o->dw_down_in : nullptr, o->ld_dw_down_in, d, f, ge);
+    const ProductPlan plan_i = c.plan(pi, {&g, &u}, {}), plan_x = c.plan(px, {}, {&dx}), plan_w = c.plan(pw, {&dwgi, &dwui}, {&dwg, &dwu}),
+                      plan_d = c.plan(pd, {&dwdi}, {&dwd});
     x.plan(c, o->dw_gate || o->dw_up);
     dy.plan(c, inner || o->dw_down);
     h.plan(c, o->dw_down);
@@ -551,6 +558,8 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     dx.plan(c, plan_x.pair, true);
     for (StandIn *s : {&dwg, &dwu}) s->plan(c, plan_w.pair, true);
     dwd.plan(c, plan_d.pair, true);
+    for (StandIn *s : {&dwgi, &dwui}) s->plan(c, plan_w.pair);
+    dwdi.plan(c, plan_d.pair);
     const int64_t ld_i = padded_ld(f, 2);
     const size_t dg_at = inner ? c.room((size_t)t * ld_i * 2) : 0, du_at = inner ? c.room((size_t)t * ld_i * 2) : 0;
     // db_gate and db_up: from the first product's epilogue, which has dg and du before they are rounded
@@ -560,12 +569,12 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
     const size_t part_at = inner_sums || o->db_down
         ? c.room((size_t)column_pass_partials(2 * f + d, c.l.sm_count) * 4) : 0;
     if ((rc = c.reserve()) != DISTSIM_OK) return rc;
-    for (StandIn *s : {&x, &dy, &h, &g, &u, &wg, &wu, &wd, &dx, &dwg, &dwu, &dwd}) s->place(c);
+    for (StandIn *s : {&x, &dy, &h, &g, &u, &wg, &wu, &wd, &dx, &dwg, &dwu, &dwd, &dwgi, &dwui, &dwdi}) s->place(c);
     const Matrix dg = inner ? mat(c.at(dg_at), ld_i) : Matrix{}, du = inner ? mat(c.at(du_at), ld_i) : Matrix{};
     float *partial = inner_sums || o->db_down ? c.at<float>(part_at) : nullptr;
     Matrix sums[2];
 
-    TRY(fetch(c, {&dy, &wd, &g, &u, &wg, &wu, &x, &h}));
+    TRY(fetch(c, {&dy, &wd, &g, &u, &wg, &wu, &x, &h, &dwgi, &dwui, &dwdi}));
     if (inner) {
         pi.a[0] = dy.use;
         pi.b[0] = wd.use;
@@ -589,21 +598,21 @@ int distsim_gated_ffn_backward(distsim_ctx *ctx, void *stream, const distsim_gat
         TRY(launch_product(c.l, px, plan_x));
     }
     if (o->dw_gate || o->dw_up) {
+        const Matrix a[2] = {dg, du}, in[2] = {dwgi.use, dwui.use}, out[2] = {dwg.use, dwu.use};
         pw.b[0] = x.use;
-        if (pw.groups == 2) {
-            pw.a[0] = dg;
-            pw.a[1] = du;
-            pw.out[0] = dwg.use;
-            pw.out[1] = dwu.use;
-        } else {
-            pw.a[0] = o->dw_gate ? dg : du;
-            pw.out[0] = o->dw_gate ? dwg.use : dwu.use;
+        for (int first = o->dw_gate ? 0 : 1; first < (o->dw_up ? 2 : 1); first += pw.groups) {
+            for (int i = 0; i < pw.groups; ++i) {
+                pw.a[i] = a[first + i];
+                pw.in[i] = in[first + i];
+                pw.out[i] = out[first + i];
+            }
+            TRY(launch_product(c.l, pw, plan_w));
         }
-        TRY(launch_product(c.l, pw, plan_w));
     }
     if (o->dw_down) {
         pd.a[0] = dy.use;
         pd.b[0] = h.use;
+        pd.in[0] = dwdi.use;
         pd.out[0] = dwd.use;
         TRY(launch_product(c.l, pd, plan_d));
     }

@@ -31,12 +31,15 @@ class _Linear(C.Structure):
                        ("x", "weight", "residual", "y", "preact", "dy", "dx", "dweight", "dweight_in"))
 
 
+_EARLIER = ("dw_gate_in", "dw_up_in", "dw_down_in")
+
+
 class _GatedFfn(C.Structure):
     _fields_ = _fields(("tokens", "d_in", "d_hidden"), ("dtype", "activation", "grad_dtype", "reserved"),
                        ("x", "w_gate", "w_up", "w_down", "b_gate", "b_up", "b_down", "residual", "y", "hidden", "gate", "up",
                         "dy", "dx", "dw_gate", "dw_up", "dw_down", "db_gate", "db_up", "db_down"),
                        ("x", "w_gate", "w_up", "w_down", "residual", "y", "hidden", "gate", "up", "dy", "dx", "dw_gate",
-                        "dw_up", "dw_down"))
+                        "dw_up", "dw_down")) + _fields((), (), _EARLIER, _EARLIER)
 
 
 class _ResidualNorm(C.Structure):
@@ -206,17 +209,20 @@ def distsim_gated_ffn_forward(ctx, x, w_gate, w_up, w_down, y, b_gate=None, b_up
 
 
 def distsim_gated_ffn_backward(ctx, dy, x, w_gate, w_up, w_down, hidden, gate, up, dx=None, dw_gate=None, dw_up=None,
-                               dw_down=None, db_gate=None, db_up=None, db_down=None, activation="silu", stream=None) -> None:
-    """Gradients of ``distsim_gated_ffn_forward`` by x, the weights and the biases (any may be None)."""
+                               dw_down=None, db_gate=None, db_up=None, db_down=None, activation="silu", dw_gate_in=None,
+                               dw_up_in=None, dw_down_in=None, stream=None) -> None:
+    """Gradients of ``distsim_gated_ffn_forward`` by x, the weights and the biases (any may be None; a weight's is
+    added to its ``dw_*_in``, if given)."""
     o, t, d, f = _ffn(ctx, x, w_gate, w_up, w_down, activation)
     o.grad_type(dw_gate, dw_up, dw_down, db_gate, db_up, db_down)
     for name, v in (("dy", dy), ("dx", dx)):
         o.matrix(name, v, t, d)
     for name, v in (("hidden", hidden), ("gate", gate), ("up", up)):
         o.matrix(name, v, t, f)
-    for name, v in (("dw_gate", dw_gate), ("dw_up", dw_up)):
+    for name, v in (("dw_gate", dw_gate), ("dw_up", dw_up), ("dw_gate_in", dw_gate_in), ("dw_up_in", dw_up_in)):
         o.matrix(name, v, f, d, o.grad)
-    o.matrix("dw_down", dw_down, d, f, o.grad)
+    for name, v in (("dw_down", dw_down), ("dw_down_in", dw_down_in)):
+        o.matrix(name, v, d, f, o.grad)
     for name, v, n in (("db_gate", db_gate, f), ("db_up", db_up, f), ("db_down", db_down, d)):
         o.vector(name, v, n, o.grad)
     o.call(_lib.distsim_gated_ffn_backward, stream)

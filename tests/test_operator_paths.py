@@ -649,6 +649,58 @@ def test_norm_gradients_one_by_one(ctx, dtype, shape, parts):
                 near((wanted, k), v, whole[k].double(), 64 * 2.0 ** -24 + (2.0 ** -10 if dtype != torch.float32 else 0))
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("plan", [0, -1, 1, 2], indirect=True)
+@pytest.mark.parametrize("shape", [(7, 100, 130, 0, 0), (300, 136, 264, 8, 0), (1300, 72, 257, 3, 1)])
+@pytest.mark.parametrize("grad", [torch.bfloat16, torch.float32])
+def test_gated_weight_gradients_added_to_earlier_ones(ctx, plan, shape, grad):
+    from paper_2306_08423_b200 import engine as E
+    t, d, f, pad, shift = shape
+    rng = np.random.default_rng(t)
+    dt = torch.bfloat16
+    o = ffn_case(rng, *shape, dt)
+    dy, g, u, h = (randn(rng, t, n, dtype=dt, pad=pad, shift=shift) for n in (d, f, f, f))
+    sizes = dict(dw_gate=(f, d), dw_up=(f, d), dw_down=(d, f))
+
+    def run(earlier, in_place=()):
+        out = {}
+        for n, (a, b) in sizes.items():
+            v, ok = room(a, b, grad, pad, shift)
+            if n in in_place:
+                v.copy_(earlier[n])
+                earlier = {**earlier, n: v}
+            out[n] = v, ok
+        E.distsim_gated_ffn_backward(ctx, dy, **o, hidden=h, gate=g, up=u, **{n: q[0] for n, q in out.items()}, activation="silu",
+                                     **{n + "_in": v for n, v in earlier.items()})
+        for _, ok in out.values():
+            ok()
+        return {n: q[0] for n, q in out.items()}
+    old = {n: randn(rng, a, b, dtype=grad, scale=t ** 0.5, pad=pad, shift=shift) for n, (a, b) in sizes.items()}
+    plain = run({})
+    whole = run(old)
+    dh = dy.double() @ o["w_down"].double()
+    dh_off = (d + 2) * U32 * dy.double().abs() @ o["w_down"].double().abs()
+    val, slope = act64(g.double(), "silu")
+    approx, x = 2.0 ** -19 * g.double().abs().clamp_min(1), o["x"].double()
+    for name, q, off in (("dw_gate", dh * u.double() * slope, u.double().abs() * (dh_off * slope.abs() + (dh.abs() + dh_off) * approx)),
+                         ("dw_up", dh * val, dh_off * val.abs() + (dh.abs() + dh_off) * approx)):
+        off = off + unit(dt) * (q.abs() + off)
+        close(name, whole[name], q.T @ x + old[name].double(), (t + 2) * U32 * (q.abs().T @ x.abs() + old[name].double().abs()) + off.T @ x.abs())
+    close("dw_down", whole["dw_down"], dy.double().T @ h.double() + old["dw_down"].double(),
+          (t + 2) * U32 * (dy.double().abs().T @ h.double().abs() + old["dw_down"].double().abs()))
+    # in place, and with some of them only
+    for names, in_place in ((sizes, sizes), (("dw_gate",), ()), (("dw_up", "dw_down"), ("dw_up",)), (("dw_gate", "dw_up"), ())):
+        for n, v in run({k: old[k] for k in names}, in_place).items():
+            if plan == 0 and n not in names:         # the choice of kernel goes by what a call reads
+                continue
+            assert torch.equal(v, (whole if n in names else plain)[n]) or plan == 0, (names, n)
+    none = torch.empty(0, d, dtype=dt, device="cuda"), torch.empty(0, f, dtype=dt, device="cuda")
+    out = {n: torch.full(s, 7.0, dtype=grad, device="cuda") for n, s in sizes.items()}
+    E.distsim_gated_ffn_backward(ctx, none[0], none[0], o["w_gate"], o["w_up"], o["w_down"], none[1], none[1], none[1], **out,
+                                 dw_gate_in=old["dw_gate"], dw_down_in=out["dw_down"])
+    assert torch.equal(out["dw_gate"], old["dw_gate"]) and not out["dw_up"].any() and bool((out["dw_down"] == 7.0).all())
+
+
 # ---------------------------------------------------------------- waits that give up
 
 @pytest.fixture
