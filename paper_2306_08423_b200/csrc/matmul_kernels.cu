@@ -89,8 +89,6 @@ struct alignas(64) ProductParams {
     int64_t sums_ld;
 };
 
-__device__ __forceinline__ uint32_t align_up(uint32_t v, uint32_t a) { return (v + a - 1) & ~(a - 1); }
-
 __device__ __forceinline__ void give_up(int32_t *status) { *reinterpret_cast<volatile int32_t *>(status) = DISTSIM_E_TIMEOUT; }
 
 // By a producer behind its last load (of `loads` so far): until every stage has been consumed, so that

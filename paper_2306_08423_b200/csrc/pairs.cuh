@@ -41,19 +41,14 @@ __device__ __forceinline__ void cut8(Oct &o, int valid, float other = 0.f)
         o.v[i] = make_pair2(2 * i < valid ? t.x : other, 2 * i + 1 < valid ? t.y : other);
     }
 }
-// EXACT: all eight exist on a 16-byte boundary.  Values beyond the row read as zero.
-template <class T, bool EXACT>
-__device__ __forceinline__ Eight<T> fetch8(const T *p, int valid, bool vec)
+// One by one; values beyond the row read as zero.
+template <class T>
+__device__ __forceinline__ Eight<T> fetch8(const T *p, int valid)
 {
     Eight<T> r;
-    if (EXACT || (vec && valid >= 8)) {
+    T *e = reinterpret_cast<T *>(r.w);
 #pragma unroll
-        for (int i = 0; i < (int)(sizeof(T) * 8 / 16); ++i) r.w[i] = *(reinterpret_cast<const uint4 *>(p) + i);
-    } else {
-        T *e = reinterpret_cast<T *>(r.w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) e[i] = i < valid ? p[i] : from_float<T>(0.f);
-    }
+    for (int i = 0; i < 8; ++i) e[i] = i < valid ? p[i] : from_float<T>(0.f);
     return r;
 }
 // Eight 2-byte values at any address of a matrix that starts at `begin` and ends before `end`: the two
@@ -87,7 +82,7 @@ __device__ __forceinline__ Oct receive8(const Request<true> &q, const T *, int) 
 template <class T>
 __device__ __forceinline__ Oct receive8(const Request<false> &q, const T *p, int valid)
 {
-    if (!q.wide) return widen(fetch8<T, false>(p, valid, false));
+    if (!q.wide) return widen(fetch8(p, valid));
     uint32_t c[8] = {q.v.x, q.v.y, q.v.z, q.v.w, q.w.x, q.w.y, q.w.z, q.w.w};
     shift_words(c, (uint32_t)reinterpret_cast<uintptr_t>(p) & 15);
     Oct o = widen(Eight<T>{{make_uint4(c[0], c[1], c[2], c[3])}});
