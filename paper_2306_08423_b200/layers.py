@@ -20,7 +20,8 @@ class FeedForward:
     [tokens, hidden]) and returns the next block's pair:
         o = act(y W1^T + b1) W2^T          (or the gated block of W_gate, W_up, W_down)
         h' = h + dropout(o);  y' = layernorm(h') weight + bias
-    ``backward(dy', dh')`` returns (dy, dh) and fills ``grads``.  With model-parallel degree mp the
+    ``backward(dy', dh')`` returns (dy, dh) and fills ``grads``.  What both return are the layer's own
+    buffers, which its next pass overwrites: they are another layer's inputs, not its own.  With model-parallel degree mp the
     shard's hidden width is ``d_hidden / mp``; o is then a partial sum that the model-parallel
     all-reduce completes (an event of its own, not run here).
     """
@@ -51,7 +52,14 @@ class FeedForward:
         self.offset = 0
         self.draws = tokens * ((hidden + 1) // 2)
 
+    def _not_own(self, **inputs):
+        own = {v.data_ptr() for v in self.outer.values()}
+        for name, v in inputs.items():
+            if v.numel() and v.data_ptr() in own:
+                raise ValueError(f"{name}: one of the layer's own buffers, which the pass overwrites; pass a copy")
+
     def forward(self, y, h, stream=None):
+        self._not_own(y=y, h=h)
         e, p, i, o = self.engine, self.params, self.inner, self.outer
         self.offset = self.step * self.draws
         self.step += 1
@@ -68,6 +76,7 @@ class FeedForward:
         return o["y"], o["h"]
 
     def backward(self, dy, dh, stream=None):
+        self._not_own(dy=dy, dh=dh)
         e, p, g, i, o = self.engine, self.params, self.grads, self.inner, self.outer
         e.distsim_residual_norm_backward(self.ctx, None, o["h"], dy=dy, dh=dh, dx=o["do"], dresidual=o["dh"], dweight=g["weight"],
                                          dbias=g["bias"], weight=p["weight"], p=self.p, seed=self.seed, offset=self.offset, stream=stream)

@@ -787,3 +787,24 @@ def test_norms_that_give_up(impatient, shape, parts):
         call()
         E.distsim_operator_status(c)
         assert all(torch.equal(a, v) for a, v in zip(first, got))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("gated", [False, True])
+def test_a_layer_refuses_its_own_buffers(ctx, gated):
+    # they would be overwritten while the pass reads them, or before the backward pass does
+    from paper_2306_08423_b200.layers import FeedForward
+    one, two = (FeedForward(ctx, 40, 64, 128, gated=gated, seed=k) for k in range(2))
+    y, h = (torch.randn(40, 64, device="cuda").bfloat16() for _ in range(2))
+    out = one.forward(y, h)
+    with pytest.raises(ValueError, match="own buffers"):
+        one.forward(out[0], h)
+    with pytest.raises(ValueError, match="own buffers"):
+        one.forward(y, out[1])
+    two.forward(*out)
+    grads = two.backward(y, h)
+    with pytest.raises(ValueError, match="own buffers"):
+        two.backward(grads[0], h)
+    with pytest.raises(ValueError, match="own buffers"):
+        two.backward(y, grads[1])
+    one.backward(*grads)
