@@ -150,7 +150,12 @@ inline cudaError_t ensure_dynamic_smem(const void *kernel, size_t bytes)
             return e;
         }
     e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e == cudaSuccess) granted.push_back(Granted{kernel, dev, bytes});
+    if (e == cudaSuccess) {
+        try {
+            granted.push_back(Granted{kernel, dev, bytes});
+        } catch (const std::bad_alloc &) {               // no exception leaves a C entry; the next launch asks again
+        }
+    }
     return e;
 }
 

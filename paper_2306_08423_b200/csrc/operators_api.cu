@@ -68,7 +68,14 @@ struct Call {
 
     explicit Call(distsim_ctx *c, void *s) : ctx(c), stream(static_cast<cudaStream_t>(s)) {}
 
-    int fail(int code, const char *text) { return a.fail(ctx, code, text); }
+    int fail(int code, const char *text)
+    {
+        try {
+            return a.fail(ctx, code, text);
+        } catch (const std::bad_alloc &) {           // the text's copy; no exception leaves a C entry
+            return code;
+        }
+    }
     int cuda(cudaError_t e, const char *what)
     {
         char text[256];

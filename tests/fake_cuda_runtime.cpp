@@ -11,6 +11,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <map>
+#include <new>
 #include <string>
 #include <utility>
 
@@ -23,10 +24,17 @@ std::map<const void *, std::string> kernels;
 std::map<std::pair<const void *, int>, int> granted;          // dynamic shared memory of (kernel, device)
 std::map<void *, size_t> blocks;
 uintptr_t next_address = 0x100000000000;
-int device = 0, launches_until_failure = -1, clusters = 10;
+int device = 0, launches_until_failure = -1, clusters = 10, allocations_until_failure = -1;
+
+struct Own {                                                  // while it lives allocations are the fake runtime's and succeed
+    int kept = allocations_until_failure;
+    Own() { allocations_until_failure = -1; }
+    ~Own() { allocations_until_failure = kept; }
+};
 
 void note(const char *format, ...)
 {
+    const Own own;
     char line[512];
     va_list a;
     va_start(a, format);
@@ -54,6 +62,17 @@ CUresult encode(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cu
 
 }  // namespace
 
+// The library's own allocations (those within the C++ library are its own).
+void *operator new(size_t n)
+{
+    if (allocations_until_failure == 0) throw std::bad_alloc();
+    if (allocations_until_failure > 0) --allocations_until_failure;
+    if (void *p = malloc(n)) return p;
+    throw std::bad_alloc();
+}
+void operator delete(void *p) noexcept { free(p); }
+void operator delete(void *p, size_t) noexcept { free(p); }
+
 extern "C" {
 
 // ---- what tests call -------------------------------------------------------------------------
@@ -67,6 +86,7 @@ const char *fake_log()                                       // the events since
 void fake_stream(void *handle, unsigned long long id, int capturing) { streams[handle] = Stream{id, capturing != 0}; }
 void fake_fail_launch(int after) { launches_until_failure = after; }
 void fake_clusters(int n) { clusters = n; }                  // that the present device holds at a time
+void fake_fail_allocations(int after) { allocations_until_failure = after; }       // -1: no more
 int fake_blocks() { return (int)blocks.size(); }
 
 // ---- the runtime -----------------------------------------------------------------------------
@@ -89,6 +109,7 @@ cudaError_t cudaDeviceGetAttribute(int *v, cudaDeviceAttr a, int)
 cudaError_t cudaDeviceGetStreamPriorityRange(int *lo, int *hi) { *lo = *hi = 0; return cudaSuccess; }
 cudaError_t cudaMalloc(void **p, size_t bytes)
 {
+    const Own own;
     *p = reinterpret_cast<void *>(next_address);
     next_address += (bytes + 4095) / 4096 * 4096 + 4096;
     blocks[*p] = bytes;
@@ -130,6 +151,7 @@ cudaError_t cudaStreamGetId(cudaStream_t s, unsigned long long *id)
 }
 cudaError_t cudaFuncSetAttribute(const void *kernel, cudaFuncAttribute a, int v)
 {
+    const Own own;
     if (a == cudaFuncAttributeMaxDynamicSharedMemorySize) granted[{kernel, device}] = v;
     return cudaSuccess;
 }

@@ -4,6 +4,7 @@ import ctypes as C
 import os
 import re
 import subprocess
+import sys
 
 import pytest
 
@@ -14,14 +15,23 @@ E_ARG, E_STATE, E_CUDA = -1, -2, -6
 @pytest.fixture(scope="module")
 def lib(tmp_path_factory):
     """The library on the fake runtime."""
+    return load(build(tmp_path_factory))
+
+
+def build(tmp_path_factory):
     from paper_2306_08423_b200 import build as B
     B.build()
     so = str(tmp_path_factory.mktemp("fake") / "libdistsim_fake.so")
     objects = [os.path.join(B._OBJ, s.replace(".cu", ".o")) for s in B.SOURCES]
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-I/usr/local/cuda/include", "-o", so,
                     os.path.join(HERE, "fake_cuda_runtime.cpp"), *objects], check=True, capture_output=True, text=True)
+    return so
+
+
+def load(so):
     from paper_2306_08423_b200 import operators as O
     f = C.CDLL(so)
+    f.path = so
     f.distsim_create.argtypes = [C.POINTER(C.c_void_p), C.c_int]
     f.distsim_destroy.argtypes = [C.c_void_p]
     f.distsim_last_error.argtypes = [C.c_void_p]
@@ -229,3 +239,25 @@ def test_a_call_that_fails_half_way_is_waited_for(lib, ctx):
     assert len(of(events, "launch")) == 2 and events[-1] == "record stream=0x20"
     ctx.backward(100, 0x10)
     assert log(lib)[0] == "wait stream=0x10"
+
+
+# ---------------------------------------------------------------- host memory
+
+def test_no_exception_leaves_a_call(lib):
+    # in a process of its own, which an exception through a C entry would end
+    code = f"""
+import sys
+sys.path.insert(0, {os.path.dirname(HERE)!r})
+from tests.test_operator_calls import Context, load
+lib = load({lib.path!r})
+ctx = Context(lib)
+for plan in (1, -2, -1):                             # kernels whose shared memory has not been asked for yet
+    assert lib.distsim_testing_set_product_plan(ctx.h, plan) == 0
+    lib.fake_fail_allocations(0)
+    ctx.backward(40, 0x10)
+    lib.fake_fail_allocations(-1)
+ctx.backward(-1, 0x10, rc=-1)
+assert ctx.error() == "linear: sizes"
+ctx.close()
+"""
+    subprocess.run([sys.executable, "-c", code], check=True)
