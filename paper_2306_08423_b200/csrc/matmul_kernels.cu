@@ -25,12 +25,12 @@
 //   are worth (the tile above takes 0.27 us a step whatever part of it is real) and shared memory
 //   holds little but the weight's stream.  The reduction is split like the split kernel's.
 //
-// Measured (bf16, of the 1669 TFLOP/s of a library product measured alone; the clock falls under the
-// power limit): persistent, 8192 x 6144 x 12288 with residual 800 to 940 us (79 to 92 %), 8192 x 1024 x
-// 4096 with gelu and its argument kept 64 to 78 us; gated block of 8192 tokens, 2048 x 8192, 590 to 680 us;
-// split, 512 x 1024 x 4096 14.5 us; few rows, 1 x 1024 x 4096 5 us, 7 tokens through a gated block of 2048 x
-// 8192 28 us (100 MB of weights).  The large ones are bound by the tensor pipe, the small ones by the fill
-// of the ring, the exchange and the last rows.
+// Measured on several chips (bf16, of the 1669 TFLOP/s of a library product measured alone; the clock falls
+// under the power limit): persistent, 8192 x 6144 -> 12288 with residual 800 to 960 us (77 to 92 %), 8192 x 1024 ->
+// 4096 57 us, with gelu and its argument kept 78 to 81 us (the epilogue of 16 steps' tile is longer than the steps);
+// gated block of 8192 tokens, 2048 x 8192, 590 to 700 us; split, 512 x 4096 -> 1024 14.5 us; few rows, 1 x 4096 -> 1024 5
+// us, 7 tokens through a gated block of 2048 x 8192 28 us (100 MB of weights).  Small ones are bound by the fill of
+// the ring, the exchange and the last rows, large ones by the tensor pipe, short reductions by the epilogue.
 //
 // Operands whose rows run over the reduction index and operands whose rows run over the output
 // index are both read as they lie in memory (the tensor core takes either order), so no weight

@@ -6,21 +6,23 @@
 // so every value is read and written once whatever the number of norms, and barriers are few; many
 // teams share an SM.  Rows come into shared memory by bulk copies: forward as soon as a tensor's part
 // of a row is in registers, the next row's is on its way; backward a row ahead, all tensors behind one
-// barrier.  Arithmetic goes in pairs of floats where both halves take the same steps: the kernels are
-// bound by instructions, a third of them dropout's generator, whose mask is computed from the counter
-// where it is needed.  Backward, a thread also keeps four sums of its columns in registers, so rows of
-// more than 4096 columns (2048 in 32 bits and backward) are held by the 2, 4 or 8 blocks of a cluster,
-// which send each other their parts of a row's sums (asynchronous stores that complete on the
-// receiver's barrier; a cluster-wide barrier would wait for the row's global stores instead), and a
+// barrier.  Arithmetic goes in pairs of floats where both halves take the same steps; dropout's mask is
+// computed from its counter where it is needed.  Instructions fill 55 to 61 % of the issue slots (DRAM: 31 to
+// 43 %), in the forward pass a third of them the generator's; the rest is waiting for a row's exchanges,
+// which few warps an SM (12 backward) do not cover.  Backward, a thread also keeps four sums of its columns
+// in registers, so rows of more than 4096 columns (2048 in 32 bits and backward) are held by the 2, 4 or 8
+// blocks of a cluster, which send each other their parts of a row's sums (asynchronous stores that complete
+// on the receiver's barrier; a cluster-wide barrier would wait for the row's global stores instead), and a
 // row's last sums go in one exchange with the next row's statistics.  Statistics are joined as (mean,
 // sum of squared distances from the mean) - the pairwise update of Chan, Golub and LeVeque - which
 // takes one exchange and does not cancel; a warp that a row fills partly takes its own in two passes.
 //
-// Measured (bf16, of the copy bandwidth of 6.46 TB/s), forward with both norms, gate and dropout of
-// 0.1: 32768 x 2048 136 us (61 %; 95 us and 88 % without dropout), 8192 x 12288 248 us, 512 x 768 (f32)
-// 5 us, of which most is a launch's and a row's latency.  Backward with all gradients: 8192 x 12288 460 us
-// (41 %), 32768 x 2048 330 us.  Rows that do not fill whole warps' pieces, forward / backward of 32768:
-// 2056 columns 198 / 511 us, 2047: 262 / 690 us (element-wise accesses: 584 / 1133 us).
+// Measured (bf16, of the copy bandwidth of 6.46 TB/s), with both norms, gate and dropout of 0.1.  Forward,
+// root-mean-square / layer norms: 32768 x 2048 136 / 147 us (61 / 57 %; 94 / 107 us without dropout), 8192 x 12288
+// 247 / 268 us.  Backward with all gradients, layer norms: 8192 x 12288 464 us (40 %), 32768 x 2048 330 us.  Rows
+// that do not fill whole warps' pieces, forward (root-mean-square) / backward (layer) of 32768: 2056 columns
+// 193 / 517 us, 2047: 258 / 703 us (element-wise accesses: 584 / 1133 us).  512 x 768 (f32) forward with the norm
+// behind only 5 us, of which most is a launch's and a row's latency.
 //
 // Backward: with m = mask / (1 - p), hat(v) = (v - mean) / sd,
 //   a = dy w2,   dH = dh + (a - mean(a) - hat(h) mean(a hat(h))) / sd_h,   dr = alpha dH,

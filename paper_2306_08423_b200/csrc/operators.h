@@ -85,9 +85,10 @@ cudaError_t launch_kernel(OperatorLaunch &l, Start start, void (*kernel)(Params.
 // How a product is run: the estimate (in microseconds, fitted to products of 1 to 8192 rows) says
 // which is faster.  A pair's step of 256 x 256 x 64 takes 0.265 us; a persistent kernel overlaps its
 // tiles' epilogues with the next products, a split one shortens the longest reduction but finishes
-// its rows after it.  Measured, persistent / split 2 / split 4 in us: 1 row x 4096 x 1024: 22.1 / 13.4
-// / 9.4;  512 x 1024 x 4096: 23.2 / 17.4 / 14.5;  gradient 768 x 768 over 8192: 41.4 / 27.1 / 19.8;
-// 1024 x 1024 x 1024: 10.0 / 10.8 / 20.3 (clusters of 8 blocks: fewer than 16 fit).
+// its rows after it.  Measured, persistent / split 1 / 2 / 4 in us (forward with bias, bf16): 100 x 4096 -> 1024
+// 23.3 / 25.7 / 17.4 / 13.4;  512 x 4096 -> 1024 23.7 / 26.8 / 17.9 / 14.5;  512 x 1024 -> 4096 10.7 / 13.8 / 12.7 / 32.0;
+// 1024 x 1024 -> 1024 10.5 / 13.4 / 11.3 / 20.9 (clusters of 8 blocks: fewer than 16 fit);  8192 x 1024 -> 4096 59 /
+// 104 / 190 / 387;  gradient 768 x 768 over 8192, persistent / split 2 / 4: 41.4 / 27.1 / 19.8.
 struct ProductPlan {
     bool pair = false;            // persistent pairs of blocks, else a cluster a tile
     bool few = false;             // tokens as the tensor core's columns (few_rows())
