@@ -93,7 +93,7 @@ struct Team {
     bool dead = false;
     int lack = 0;                                // columns that this warp could hold and the row does not have
     int phase;                                   // values that the team's pieces start before its columns
-    float inv_n;                                 // 1 / columns of a row
+    float cols, inv_n;                           // columns of a row, and 1 / that
     float weight = 0.f;                          // columns of the warp whose entry the lane joins
 
     // row_arrivals: of the barrier of a row's copies
@@ -107,7 +107,8 @@ struct Team {
         scratch = all + id;
         status = p.status;
         polls = p.polls;
-        inv_n = 1.f / (float)p.cols;
+        cols = (float)p.cols;
+        inv_n = 1.f / cols;
         phase = (int)(((p.ref_start + (uint32_t)((blockIdx.x / p.cluster) * p.teams + id) * p.ref_pitch) & 15) >> p.ref_shift);
         if (thread == 0) {
             for (int i = 0; i < 2; ++i) mbar_init(smem_addr(&scratch->arrived[i]), 1);
@@ -212,6 +213,12 @@ struct Team {
         ++exchanges;
         return entry;
     }
+    // v / columns of a row, as division rounds it: the mean of a row of equal values is their value.
+    __device__ __forceinline__ float divided(float v) const
+    {
+        const float q = v * inv_n;
+        return fmaf(fmaf(-q, cols, v), inv_n, q);
+    }
     // Joins the warps' entries (sums, or moments); every warp does so for itself.
     template <int N, bool MOMENTS>
     __device__ __forceinline__ float4 join_entries(const float4 *entry) const
@@ -224,8 +231,8 @@ struct Team {
 #pragma unroll
         for (int o = kMaxEntries / 2; o > 0; o >>= 1) v = add<N>(v, shuffle<N>(v, o));
         if (MOMENTS) {
-            v.x *= inv_n;
-            v.z *= inv_n;
+            v.x = divided(v.x);
+            if (N > 2) v.z = divided(v.z);
             const float d = own.x - v.x, e = own.z - v.z;
             float4 q = make_float4(d * d * n, e * e * n, 0.f, 0.f);
 #pragma unroll
@@ -638,12 +645,12 @@ __device__ __forceinline__ Oct times8(const Oct &a, const Oct &b)
     for (int i = 0; i < 4; ++i) r.v[i] = mul2(a.v[i], b.v[i]);
     return r;
 }
-// v * scale + shift: (v - mean) / sd with scale = 1 / sd, shift = -mean / sd.
-__device__ __forceinline__ void shift8(Oct &v, float scale, float shift)
+// (v - mean) * scale, in this order: a row of equal values becomes zeros, not what rounding mean * scale leaves.
+__device__ __forceinline__ void centre8(Oct &v, float mean, float scale)
 {
-    const Pair s = both(scale), t = both(shift);
+    const Pair s = both(scale), m = both(-mean);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v.v[i] = fma2(v.v[i], s, t);
+    for (int i = 0; i < 4; ++i) v.v[i] = mul2(add2(v.v[i], m), s);
 }
 // v * weight + bias
 template <class P, class TEAM>
@@ -697,7 +704,7 @@ residual_norm_forward_kernel(const __grid_constant__ NormParams p)
             x.start(team, row + stride);
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                shift8(v[j], rstd, -mean * rstd);
+                centre8(v[j], mean, rstd);
                 affine8(v[j], team, w1, b1, j);
             }
         }
@@ -736,7 +743,7 @@ residual_norm_forward_kernel(const __grid_constant__ NormParams p)
             T *y = (T *)p.y + row * p.ld_y + c;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
-                shift8(v[j], rstd, -mean * rstd);
+                centre8(v[j], mean, rstd);
                 affine8(v[j], team, w2, b2, j);
                 write_columns<T, L>(y + j * step, j == 0 ? lead : 0, valid - j * step, v[j]);
             }
@@ -802,7 +809,7 @@ residual_norm_backward_kernel(const __grid_constant__ NormParams p)
                 team.template trim_read<L>(dh, valid);
 #pragma unroll
                 for (int j = 0; j < NV; ++j) {
-                    shift8(hat[j], rstd[0], -mean[0] * rstd[0]);
+                    centre8(hat[j], mean[0], rstd[0]);
                     const Oct w = w2.read(team, j), f = dh[j];                       // zero beyond the row
                     const Oct t = times8(f, hat[j]);
                     dh[j] = times8(f, w);
@@ -845,7 +852,7 @@ residual_norm_backward_kernel(const __grid_constant__ NormParams p)
                 team.template trim_read<L>(hat, valid);
                 if (p.w1)
 #pragma unroll
-                    for (int j = 0; j < NV; ++j) shift8(hat[j], rstd_x, -mean_x * rstd_x);
+                    for (int j = 0; j < NV; ++j) centre8(hat[j], mean_x, rstd_x);
             }
             if (p.threshold) {
 #pragma unroll

@@ -701,6 +701,32 @@ def test_gated_weight_gradients_added_to_earlier_ones(ctx, plan, shape, grad):
     assert torch.equal(out["dw_gate"], old["dw_gate"]) and not out["dw_up"].any() and bool((out["dw_down"] == 7.0).all())
 
 
+# ---------------------------------------------------------------- rows of equal values
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("cols,shift", [(1, 0), (2, 1), (3, 0), (100, 0), (256, 0), (768, 0), (1000, 0), (2047, 0), (2048, 0), (4104, 0), (5000, 1), (12288, 0),
+                                        (16384, 0), (16381, 0)])
+def test_layer_norm_of_equal_values_is_its_bias(ctx, dtype, cols, shift):
+    # values of 8 digits: their sums are exact in the 24 of 32 bits (at most 2^14 of them), so their distance from the mean is zero, and so is all that follows
+    from paper_2306_08423_b200 import engine as E
+    rng = np.random.default_rng(cols)
+    value = torch.tensor([3.0, -0.6875, 100.0, 1.0, 0.01, -29.0, 0.0], device="cuda").bfloat16().to(dtype)
+    x = randn(rng, 7, cols, dtype=dtype, shift=shift)
+    x.copy_(value[:, None].expand(7, cols))
+    w, b, w2, b2 = (randn(rng, cols, dtype=dtype) for _ in range(4))
+    h, y = (torch.full((7, cols), 9.0, dtype=dtype, device="cuda") for _ in range(2))
+    E.distsim_residual_norm_forward(ctx, x, h=h, y=y, post_weight=w, post_bias=b, weight=w2, bias=b2)
+    assert torch.equal(h, b.expand(7, cols))
+    E.distsim_residual_norm_forward(ctx, x, y=y, weight=w2, bias=b2)
+    assert torch.equal(y, b2.expand(7, cols))
+    dy, dx, dw, dw2 = randn(rng, 7, cols, dtype=dtype), torch.empty_like(h), torch.ones_like(w), torch.ones_like(w)
+    E.distsim_residual_norm_backward(ctx, x, x, dy=dy, dx=dx, dweight=dw2, dpost_weight=dw, weight=w2, post_weight=w)
+    assert not dw.any() and not dw2.any()
+    if cols == 1:
+        assert not dx.any()
+
+
 # ---------------------------------------------------------------- waits that give up
 
 @pytest.fixture
