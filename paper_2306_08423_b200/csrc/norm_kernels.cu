@@ -7,8 +7,8 @@
 // teams share an SM.  Rows come into shared memory by bulk copies: forward as soon as a tensor's part
 // of a row is in registers, the next row's is on its way; backward a row ahead, all tensors behind one
 // barrier.  Arithmetic goes in pairs of floats where both halves take the same steps; dropout's mask is
-// computed from its counter where it is needed.  Instructions fill 55 to 61 % of the issue slots (DRAM: 31 to
-// 43 %), in the forward pass a third of them the generator's; the rest is waiting for a row's exchanges,
+// computed from its counter where it is needed.  Instructions fill 55 to 62 % of the issue slots (DRAM: 31 to
+// 42 %), in the forward pass a third of them the generator's; the rest is waiting for a row's exchanges,
 // which few warps an SM (12 backward) do not cover.  Backward, a thread also keeps four sums of its columns
 // in registers, so rows of more than 4096 columns (2048 in 32 bits and backward) are held by the 2, 4 or 8
 // blocks of a cluster, which send each other their parts of a row's sums (asynchronous stores that complete
@@ -18,10 +18,10 @@
 // takes one exchange and does not cancel; a warp that a row fills partly takes its own in two passes.
 //
 // Measured (bf16, of the copy bandwidth of 6.46 TB/s), with both norms, gate and dropout of 0.1.  Forward,
-// root-mean-square / layer norms: 32768 x 2048 136 / 147 us (61 / 57 %; 94 / 107 us without dropout), 8192 x 12288
-// 247 / 268 us.  Backward with all gradients, layer norms: 8192 x 12288 464 us (40 %), 32768 x 2048 330 us.  Rows
+// root-mean-square / layer norms: 32768 x 2048 138 / 149 us (60 / 56 %; 98 / 109 us without dropout), 8192 x 12288
+// 249 / 271 us.  Backward with all gradients, layer norms: 8192 x 12288 471 us (40 %), 32768 x 2048 336 us.  Rows
 // that do not fill whole warps' pieces, forward (root-mean-square) / backward (layer) of 32768: 2056 columns
-// 193 / 517 us, 2047: 258 / 703 us (element-wise accesses: 584 / 1133 us).  512 x 768 (f32) forward with the norm
+// 195 / 522 us, 2047: 260 / 704 us (element-wise accesses: 584 / 1133 us).  512 x 768 (f32) forward with the norm
 // behind only 5 us, of which most is a launch's and a row's latency.
 //
 // Backward: with m = mask / (1 - p), hat(v) = (v - mean) / sd,
