@@ -26,8 +26,8 @@
 //   holds little but the weight's stream.  The reduction is split like the split kernel's.
 //
 // Measured on several chips (bf16, of the 1669 TFLOP/s of a library product measured alone; the clock falls
-// under the power limit): persistent, 8192 x 6144 -> 12288 with residual 800 to 960 us (77 to 92 %), 8192 x 1024 ->
-// 4096 57 us, with gelu and its argument kept 78 to 81 us (the epilogue of 16 steps' tile is longer than the steps);
+// under the power limit): persistent, 8192 x 6144 -> 12288 with residual 800 to 972 us (76 to 92 %), 8192 x 1024 ->
+// 4096 57 us, with gelu and its argument kept 67 to 81 us (the epilogue of 16 steps' tile is longer than the steps);
 // gated block of 8192 tokens, 2048 x 8192, 590 to 700 us; split, 512 x 4096 -> 1024 14.5 us; few rows, 1 x 4096 -> 1024 5
 // us, 7 tokens through a gated block of 2048 x 8192 28 us (100 MB of weights).  Small ones are bound by the fill of
 // the ring, the exchange and the last rows, large ones by the tensor pipe, short reductions by the epilogue.
