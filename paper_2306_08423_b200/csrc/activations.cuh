@@ -87,9 +87,10 @@ __device__ __forceinline__ float min_or_nan(float a, float b)
 // The normal distribution function's tail at -|z|, negated, with |z| (cut to 10000: its tail is zero, and
 // infinity would make their product no number) and exp(-z^2 / 2).  The tail is exp(-z^2 / 2) times a
 // function that falls slowly, as t times a polynomial in t = 1 / (1 + 0.3 |z|) (the form of Hastings,
-// "Approximations for Digital Computers", 1955), fitted here over 0 <= |z| <= 14.5 by least squares of the relative error, reweighted towards the largest (1.6e-7).  So both tails keep
-// their digits: off by 2.4e-7 absolutely, and of itself by 6e-7 down to -2, 2e-6 down to -6, 8e-6 down to
-// -13 (the exponential's argument is rounded), where it is below the smallest 32-bit number.
+// "Approximations for Digital Computers", 1955), fitted here over 0 <= |z| <= 14.5 by least squares of the
+// relative error, reweighted towards the largest (1.6e-7).  So both tails keep their digits: off by 2.4e-7
+// absolutely, and of itself by 6e-7 down to -2, 2e-6 down to -6, 8e-6 down to -13 (the exponential's argument
+// is rounded), where it is below the smallest 32-bit number.
 // It costs an exponential more than 1/2 + z P(z^2) / Q(z^2), which is exact to 3.3e-7 absolutely only (4 %
 // off at -4.5): 8192 x 1024 -> 4096 with its argument kept 80.9 against 78.2 us, in turn.
 __device__ __forceinline__ Pair normal_tail(Pair z, Pair &size, Pair &bell)
